@@ -359,6 +359,87 @@ ADPSGD_API const char *adpsgd_last_error(void);
 ADPSGD_API int adpsgd_average_noalloc(int32_t K, int64_t P, int64_t row_stride, const int64_t *tensor_offsets,
                                       int32_t T, float *x, double *var_out, void *stream);
 
+/* ---- microscaled messages ---------------------------------------------------- */
+
+/* What a worker sends at a synchronization, in 4 or 8 bits an element, and what
+ * is done with it.  A row is one worker's difference from the model that all
+ * workers share (base).  Blocks of 32 consecutive elements of a row share a
+ * scale, a power of two 2^(byte - 127); byte 255 makes the whole block NaN.
+ *
+ * These calls need no context, allocate nothing, wait for nothing and keep
+ * nothing, so they can be recorded into a HIP graph.  They run on `stream`
+ * (NULL: the null stream) of the current device, where all their memory lies. */
+#define ADPSGD_MX_E2M1 0  /* 4 bits, +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}; element 2j is in a byte's low half */
+#define ADPSGD_MX_E4M3 1  /* 8 bits, up to +-448, least 2^-9 */
+
+/* K rows of P elements in device memory.  Row k's codes are 16 (E2M1) or 32
+ * (E4M3) bytes a block at codes + k * code_stride, its scale bytes one a block
+ * at scales + k * scale_stride; a row has ceil(P / 32) blocks.  Strides are in
+ * bytes and multiples of 16, and both pointers are 16-byte aligned.  In a last
+ * block that passes P the further elements are written as zero and not used. */
+typedef struct {
+    void *codes;
+    void *scales;
+    int64_t code_stride;
+    int64_t scale_stride;
+    int64_t P;           /* >= 0                                    */
+    int32_t K;           /* in [1, 65536], K * P below 2^41         */
+    int32_t format;      /* ADPSGD_MX_*                             */
+} adpsgd_mx_rows;
+
+/* Row strides (bytes) to use for P parameters: the least odd number of 256-byte
+ * units that holds a row (0 for P <= 0 or an unknown format). */
+ADPSGD_API int64_t adpsgd_mx_code_stride(int32_t format, int64_t P);
+ADPSGD_API int64_t adpsgd_mx_scale_stride(int64_t P);
+
+/* Round d = (x - base) + residual_in to the format, every sum rounded to fp32:
+ * a block's scale is the least power of two (at least 2^-127) that brings its
+ * largest magnitude to at most 6 (E2M1) or 448 (E4M3), and an element the
+ * nearest of the format's numbers that fp32 holds, ties to even.  residual_out = d - what was sent
+ * (the error that the next message makes up for).  A block that holds a NaN or
+ * an infinity is sent as NaN and leaves no residual.
+ * x [K][P] and the residuals [K][P] have rows x_stride and residual_stride
+ * elements apart (0: P); base is [P].  base, residual_in (counted as zero) and
+ * residual_out may be NULL; residual_out may be residual_in, else it overlaps no input. */
+ADPSGD_API int adpsgd_mx_quantize(const adpsgd_mx_rows *out, const float *x, int64_t x_stride, const float *base,
+                                  const float *residual_in, float *residual_out, int64_t residual_stride,
+                                  void *stream);
+
+/* y [K][P] (rows y_stride elements apart, 0: P) = base + what was sent; base
+ * [P] may be NULL and does not overlap y. */
+ADPSGD_API int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *base, float *y, int64_t y_stride,
+                                    void *stream);
+
+/* The synchronization from messages: base_out [P] = base + the mean of the K
+ * rows (one rounding to fp32), also written to every row of x [K][P] (rows
+ * x_stride apart, 0: P), and var[tau] (device, [T]) = (1/K) sum_k sum_{i in
+ * tau} (mean_i - row_k,i)^2 in 64 bits, as adpsgd_average's of the replicas base
+ * + row.  base, base_out and x may be NULL; base_out may be
+ * base; else no two of them overlap.
+ * tensor_offsets[T+1] is in device memory, as for adpsgd_init (T in [1, 2^24]);
+ * its values are not read back: others than offsets[0] = 0 <= ... <=
+ * offsets[T] = P give wrong sums, but touch nothing outside the arrays.
+ * workspace: adpsgd_mx_average_workspace bytes of device memory, 256-byte
+ * aligned, in use until the call's work has finished: calls that may overlap
+ * need one each. */
+ADPSGD_API size_t adpsgd_mx_average_workspace(int32_t K, int64_t P, int32_t T);
+ADPSGD_API int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const int64_t *tensor_offsets,
+                                 const float *base, float *base_out, float *x, int64_t x_stride, double *var,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* out [T][K][K]: for every tensor tau the inner products sum_{i in tau} a_j,i
+ * b_k,i of the rows of two sets of messages of the same format, K <= 256 and P
+ * (b NULL or a itself: of one set with itself, a symmetric matrix; then
+ * (tr C - 1'C1 / K) / K is adpsgd_mx_average's variance).  Sums of up to 16384
+ * products are taken in fp32, the rest in 64 bits.  An E4M3 element below
+ * 2^-126 counts as zero.  tensor_offsets and workspace
+ * (adpsgd_mx_product_workspace bytes) as above.  Both workspace functions
+ * return 0 for invalid arguments. */
+ADPSGD_API size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T);
+ADPSGD_API int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *b, int32_t T,
+                                 const int64_t *tensor_offsets, float *out, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
 /* ---- generator dumps ---------------------------------------------------------- */
 
 /* c3 = 0 (the noise) runs the device code of the steps, any other tag that of the

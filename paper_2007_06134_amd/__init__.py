@@ -12,7 +12,7 @@ import numpy as np
 
 from ._native import (  # noqa: F401
     AdpsgdError, EDEVICE, EINVAL, ENONFINITE, ESTATE, EXPORTED, LAUNCH_DEVICE, LAUNCH_HOST, LAUNCH_HYBRID,
-    LIB_PATH, LR_CONST, LR_COSINE, adpsgd_average_noalloc,
+    LIB_PATH, LR_CONST, LR_COSINE, MX_E2M1, MX_E4M3, adpsgd_average_noalloc, adpsgd_mx_rows,
     LR_STEP, LR_WARMUP_STEP, OK, PERIOD_ADAPTIVE, PERIOD_ALG1, PERIOD_CONST, adpsgd_average, adpsgd_buffers, adpsgd_destroy,
     adpsgd_get_state, adpsgd_get_timing, adpsgd_hparams, adpsgd_init, adpsgd_last_error,
     adpsgd_local_steps, adpsgd_lr, adpsgd_normal_dump, adpsgd_philox_dump, adpsgd_reset, adpsgd_run,
@@ -22,6 +22,7 @@ from ._native import (  # noqa: F401
     adpsgd_padded_row_stride, adpsgd_state, adpsgd_step_average, adpsgd_sync_rec, adpsgd_timing,
     adpsgd_workspace_bytes, make_hparams,
 )
+from .mx import MxRows, mx_average, mx_dequantize, mx_product, mx_quantize  # noqa: F401
 
 
 def hparams_of(w) -> adpsgd_hparams:
@@ -85,6 +86,9 @@ class Adpsgd:
                                   xstar=self.xstar.data_ptr(), workspace=self.workspace.data_ptr(),
                                   workspace_bytes=nbytes, stream=self.stream.cuda_stream,
                                   row_stride=self.row_stride)
+        # the state of average_mx (made by its first call)
+        self.mx_base = self.mx_residual = None
+        self._mx_rows = self._mx_offsets = None
         with torch.cuda.device(self.device):
             self.ctx = adpsgd_init(self.K, self.P, off, hp, self.buf)
 
@@ -102,6 +106,39 @@ class Adpsgd:
     def step_average(self) -> np.ndarray:
         return adpsgd_step_average(self.ctx, self.T)
 
+    def average_mx(self, format: int = MX_E2M1, error_feedback: bool = True, products: bool = False):
+        """The synchronization with microscaled messages in place of fp32 replicas: every worker sends
+        its difference from mx_base, the model after the last such sync (0 at first, as the replicas),
+        in `format`; all replicas become mx_base + the mean of what was sent, which is the new mx_base.
+        With error_feedback what a worker's message left out (mx_residual) is added to its next one.
+
+        Returns the per-tensor variances of what was sent, for ``schedule`` (and, with products, the
+        workers' inner products [T, K, K] as ``mx_product`` gives them).  Like ``average`` it restarts
+        the counter and waits for the stream; momentum stays local (with avg_momentum it is refused).
+        mx_base and mx_residual belong to a checkpoint, next to x and m; reset() zeroes them."""
+        torch = self.torch
+        if self.hp.avg_momentum:
+            raise ValueError("average_mx keeps the momentum local; the hyper-parameters ask for avg_momentum")
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            if self.mx_base is None:
+                self.mx_base = torch.zeros((self.P,), device=self.device)
+            if error_feedback and self.mx_residual is None:
+                self.mx_residual = torch.zeros_like(self._x_rows)[:, :self.P]
+            if self._mx_rows is None or self._mx_rows.format != format:
+                self._mx_rows = MxRows.empty(self.K, self.P, format, self.device)
+            if self._mx_offsets is None:
+                self._mx_offsets = torch.from_numpy(self.offsets).to(self.device)
+            st = self.get_state()
+            st.cnt = 0
+            self.set_state(st)
+            rows = mx_quantize(self.x, self.mx_base, self.mx_residual if error_feedback else None, out=self._mx_rows)
+            c = mx_product(rows, self._mx_offsets) if products else None
+            _, var = mx_average(rows, self._mx_offsets, self.mx_base, x=self.x, base_out=self.mx_base)
+            out = var.cpu().numpy()
+            if c is not None:
+                out = (out, c.cpu().numpy())
+        return out
+
     def schedule(self, var: np.ndarray) -> int:
         return adpsgd_schedule(self.ctx, var)
 
@@ -113,6 +150,10 @@ class Adpsgd:
 
     def reset(self) -> None:
         adpsgd_reset(self.ctx)
+        with self.torch.cuda.stream(self.stream):
+            for t in (self.mx_base, self.mx_residual):
+                if t is not None:
+                    t.zero_()
 
     # -- state, timing
     def get_state(self) -> adpsgd_state:

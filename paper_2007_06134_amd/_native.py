@@ -23,6 +23,7 @@ OK, EINVAL, ESTATE, EDEVICE, ENONFINITE = 0, -1, -2, -3, -4
 LR_CONST, LR_STEP, LR_COSINE, LR_WARMUP_STEP = 0, 1, 2, 3
 PERIOD_CONST, PERIOD_ADAPTIVE, PERIOD_ALG1 = 0, 1, 2
 LAUNCH_HYBRID, LAUNCH_DEVICE, LAUNCH_HOST = 0, 1, 2
+MX_E2M1, MX_E4M3 = 0, 1
 
 
 class AdpsgdError(RuntimeError):
@@ -73,6 +74,11 @@ class adpsgd_timing(C.Structure):
                 ("segsum_ms", C.c_double), ("segsum_launches", C.c_int64),
                 ("trace_ms", C.c_double), ("trace_launches", C.c_int64),
                 ("graph_captures", C.c_int64), ("graph_replays", C.c_int64)]
+
+
+class adpsgd_mx_rows(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("code_stride", C.c_int64),
+                ("scale_stride", C.c_int64), ("P", C.c_int64), ("K", C.c_int32), ("format", C.c_int32)]
 
 
 from . import build as _build  # noqa: E402
@@ -131,6 +137,17 @@ _SIGS = {
     "adpsgd_last_error": (C.c_char_p, []),
     "adpsgd_average_noalloc": (C.c_int, [C.c_int32, C.c_int64, C.c_int64, _I64P, C.c_int32, C.c_void_p, _DP,
                                          C.c_void_p]),
+    "adpsgd_mx_code_stride": (C.c_int64, [C.c_int32, C.c_int64]),
+    "adpsgd_mx_scale_stride": (C.c_int64, [C.c_int64]),
+    "adpsgd_mx_quantize": (C.c_int, [C.POINTER(adpsgd_mx_rows), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_int64, C.c_void_p]),
+    "adpsgd_mx_dequantize": (C.c_int, [C.POINTER(adpsgd_mx_rows), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "adpsgd_mx_average_workspace": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int32]),
+    "adpsgd_mx_average": (C.c_int, [C.POINTER(adpsgd_mx_rows), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                    C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "adpsgd_mx_product_workspace": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int32]),
+    "adpsgd_mx_product": (C.c_int, [C.POINTER(adpsgd_mx_rows), C.POINTER(adpsgd_mx_rows), C.c_int32, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "adpsgd_philox_dump": (C.c_int, [C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32, C.c_int64,
                                      C.c_int64, C.c_void_p, C.c_void_p]),
     "adpsgd_normal_dump": (C.c_int, [C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32, C.c_int64,
