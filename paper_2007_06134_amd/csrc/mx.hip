@@ -35,7 +35,7 @@ constexpr int32_t kMaxT = 1 << 24;
 constexpr int32_t kMaxProductK = 256;
 // Blocks a launch has at most; the kernels stride over the rest.  A multiple of
 // 8, so that a block's chunks stay on its XCD.
-constexpr uint32_t kMaxGrid = 1u << 22;
+constexpr uint32_t kMaxGrid = 1u << 23;
 constexpr int64_t kMaxPieces = (int64_t(1) << 31) - 1;
 
 // Rows need not be 16-byte aligned: the hardware takes a 16-byte access at any
@@ -135,21 +135,29 @@ __device__ __forceinline__ double block_sum(double v, double *lds) {
     __syncthreads();
     double t = 0.0;
     if (threadIdx.x == 0)
-        for (int w = 0; w < kThreads / 64; ++w) t += lds[w];
+        for (uint32_t w = 0; w < blockDim.x / 64; ++w) t += lds[w];
     __syncthreads();
     return t;
 }
 
+// A float4 group of a row.  NT: past the caches, for rows that they would not
+// keep.  Full: the caller knows that the group ends by the row's end.
+template <bool NT, bool Full>
 __device__ __forceinline__ f4 load4(const float *p, int64_t e, int64_t P) {
-    if (e + 4 <= P) return *reinterpret_cast<const f4 *>(p + e);
+    if (Full || e + 4 <= P) {
+        if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const f4 *>(p + e));
+        return *reinterpret_cast<const f4 *>(p + e);
+    }
     f4 v = {0.f, 0.f, 0.f, 0.f};
     for (int j = 0; j < 4; ++j)
         if (e + j < P) v[j] = p[e + j];
     return v;
 }
+template <bool NT, bool Full>
 __device__ __forceinline__ void store4(float *p, int64_t e, int64_t P, f4 v) {
-    if (e + 4 <= P) {
-        *reinterpret_cast<f4 *>(p + e) = v;
+    if (Full || e + 4 <= P) {
+        if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<f4 *>(p + e));
+        else *reinterpret_cast<f4 *>(p + e) = v;
         return;
     }
     for (int j = 0; j < 4; ++j)
@@ -157,27 +165,36 @@ __device__ __forceinline__ void store4(float *p, int64_t e, int64_t P, f4 v) {
 }
 
 // ---- quantize, dequantize ---------------------------------------------------
-// Blocks are dealt to the XCDs round-robin: the K rows' blocks of one piece of
-// the row follow one another on one XCD, whose L2 then holds base for them.
+// A wave takes pieces of kPiece elements of one row, the kilobyte that its
+// lanes' float4 groups are.  Blocks are dealt to the XCDs round-robin, and so
+// are a row's pieces; an XCD takes `run` of its pieces of one row, then the
+// same pieces of the next row, so that base comes from memory once and from
+// that XCD's L2 for the other rows.
+constexpr int kPiece = 256;
 struct RowGrid {
     uint32_t K;
-    uint32_t pieces;       // of a row
+    uint32_t slots;        // of a row: groups of spread NU pieces
     uint32_t blocks;       // virtual blocks of the launch
     uint32_t spread;       // 8: pieces dealt to XCDs; 1: too few pieces for that
+    uint32_t run;
 };
-RowGrid row_grid(int32_t K, int64_t P, int64_t piece) {
+RowGrid row_grid(int32_t K, int64_t P, int nu) {
     RowGrid g;
+    const int64_t pieces = (P + kPiece - 1) / kPiece;
     g.K = (uint32_t)K;
-    g.pieces = (uint32_t)((P + piece - 1) / piece);
-    g.spread = g.pieces >= 8 ? 8 : 1;
-    g.blocks = (g.pieces + g.spread - 1) / g.spread * g.spread * g.K;
+    g.spread = pieces >= 8 ? 8 : 1;
+    g.slots = (uint32_t)((pieces + g.spread * nu - 1) / (g.spread * nu));
+    g.run = g.slots >= 128u / nu ? 32u / nu : 1;
+    g.blocks = (g.slots + g.run - 1) / g.run * g.run * g.spread * g.K;
     return g;
 }
-__device__ __forceinline__ bool row_piece(const RowGrid &g, uint32_t b, uint32_t *k, uint32_t *piece) {
-    const uint32_t s = b / g.spread;
-    *k = s % g.K;
-    *piece = s / g.K * g.spread + b % g.spread;
-    return *piece < g.pieces;
+// Block b's row and first piece (its further ones lie spread apart).
+__device__ __forceinline__ bool row_piece(const RowGrid &g, int nu, uint32_t b, uint32_t *k, uint32_t *piece) {
+    const uint32_t s = b / g.spread, run = s / g.run;
+    *k = run % g.K;
+    const uint32_t slot = run / g.K * g.run + s % g.run;
+    *piece = slot * nu * g.spread + b % g.spread;
+    return slot < g.slots;
 }
 
 struct QuantizeParams {
@@ -194,53 +211,54 @@ struct QuantizeParams {
 
 // One lane holds four elements of a block, eight lanes a block.  Elements past
 // the row's end count as zero and are sent as such.
-template <int F, int NU>
-__global__ void __launch_bounds__(kThreads) k_mx_quantize(QuantizeParams p) {
+template <int F, bool NT, bool Full>
+__device__ __forceinline__ void quantize_piece(const QuantizeParams &p, uint32_t k, int64_t e) {
     using Code = typename Fmt<F>::Code;
-    const int64_t padded = (p.P + kMxBlock - 1) / kMxBlock * kMxBlock;
+    f4 d = load4<NT, Full>(p.x + k * p.x_ld, e, p.P);
+    f4 b = {0.f, 0.f, 0.f, 0.f}, r = {0.f, 0.f, 0.f, 0.f};
+    if (p.base) b = load4<false, Full>(p.base, e, p.P);
+    if (p.r_in) r = load4<NT, Full>(p.r_in + k * p.r_ld, e, p.P);
+    if (p.base) d -= b;
+    if (p.r_in) d += r;
+    // (lanes of one block are all past the padded row's end or none is)
+    if (!Full && e >= (p.P + kMxBlock - 1) / kMxBlock * kMxBlock) return;
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t a = __float_as_uint(d[j]) & 0x7fffffffu;
+        m = a > m ? a : m;
+    }
+    m = max_of_8_lanes(m);
+    // the least power of two that holds the largest element
+    const int32_t s = (int32_t)(m >> 23) - Fmt<F>::kTopExp + ((m & 0x7fffffu) > Fmt<F>::kTopMan ? 1 : 0);
+    uint32_t byte = (uint32_t)(s > 0 ? s : 0);
+    f4 v = d;
+    float scale = scale_of(byte);
+    if (m >= __float_as_uint(Fmt<F>::kMost)) {
+        if (m >= 0x7f800000u) {      // a NaN or an infinity: nothing of the block can be sent
+            byte = 255;
+            scale = 1.f;
+            d = v = f4{0.f, 0.f, 0.f, 0.f};
+        } else {                     // the format's next number is 2^128
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = fminf(fmaxf(v[j], -Fmt<F>::kMost), Fmt<F>::kMost);
+        }
+    }
+    const uint32_t c = Fmt<F>::encode(v, scale);
+    *reinterpret_cast<Code *>(p.codes + k * p.code_ld + (e >> 2) * sizeof(Code)) = (Code)c;
+    if ((threadIdx.x & 7) == 0) p.scales[k * p.scale_ld + (e >> 5)] = (uint8_t)byte;
+    if (p.r_out && (Full || e < p.P))
+        store4<NT, Full>(p.r_out + k * p.r_ld, e, p.P, d - Fmt<F>::decode(c, scale));
+}
+
+template <int F, bool NT>
+__global__ void __launch_bounds__(64) k_mx_quantize(QuantizeParams p) {
     for (uint32_t b = blockIdx.x; b < p.g.blocks; b += gridDim.x) {
         uint32_t k, piece;
-        if (!row_piece(p.g, b, &k, &piece)) continue;
-        const int64_t e0 = (int64_t)piece * (kThreads * 4 * NU) + threadIdx.x * 4;
-        const float *x = p.x + k * p.x_ld;
-        f4 d[NU];
-#pragma unroll
-        for (int u = 0; u < NU; ++u) d[u] = load4(x, e0 + u * (kThreads * 4), p.P);
-        if (p.base) {
-#pragma unroll
-            for (int u = 0; u < NU; ++u) d[u] -= load4(p.base, e0 + u * (kThreads * 4), p.P);
-        }
-        if (p.r_in) {
-#pragma unroll
-            for (int u = 0; u < NU; ++u) d[u] += load4(p.r_in + k * p.r_ld, e0 + u * (kThreads * 4), p.P);
-        }
-#pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            const int64_t e = e0 + u * (kThreads * 4);
-            if (e >= padded) continue;          // (whole blocks: the lanes of one agree)
-            uint32_t m = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t a = __float_as_uint(d[u][j]) & 0x7fffffffu;
-                m = a > m ? a : m;
-            }
-            m = max_of_8_lanes(m);
-            // the least power of two that holds the largest element
-            const int32_t s = (int32_t)(m >> 23) - Fmt<F>::kTopExp + ((m & 0x7fffffu) > Fmt<F>::kTopMan ? 1 : 0);
-            const bool bad = m >= 0x7f800000u;   // a NaN or an infinity: nothing of the block can be sent
-            const uint32_t byte = bad ? 255u : (uint32_t)(s > 0 ? s : 0);
-            f4 v = d[u];
-            if (bad) v = f4{0.f, 0.f, 0.f, 0.f};
-            else if (byte == 255u - Fmt<F>::kTopExp) {     // (the next number up would be 2^128)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = fminf(fmaxf(v[j], -Fmt<F>::kMost), Fmt<F>::kMost);
-            }
-            const float scale = bad ? 1.f : scale_of(byte);
-            const uint32_t c = Fmt<F>::encode(v, scale);
-            *reinterpret_cast<Code *>(p.codes + k * p.code_ld + (e >> 2) * sizeof(Code)) = (Code)c;
-            if ((threadIdx.x & 7) == 0) p.scales[k * p.scale_ld + (e >> 5)] = (uint8_t)byte;
-            if (p.r_out && e < p.P) store4(p.r_out + k * p.r_ld, e, p.P, (bad ? v : d[u]) - Fmt<F>::decode(c, scale));
-        }
+        if (!row_piece(p.g, 1, b, &k, &piece)) continue;
+        const int64_t e0 = (int64_t)piece * kPiece, e = e0 + threadIdx.x * 4;
+        if (e0 + kPiece <= p.P) quantize_piece<F, NT, true>(p, k, e);
+        else quantize_piece<F, NT, false>(p, k, e);
     }
 }
 
@@ -251,32 +269,46 @@ struct DequantizeParams {
     float *y;
     int64_t y_ld, code_ld, scale_ld;
     int64_t P;
-    RowGrid g;
+    int32_t K;
+    uint32_t groups, blocks, spread;
 };
 
-template <int F, int NU>
-__global__ void __launch_bounds__(kThreads) k_mx_dequantize(DequantizeParams p) {
+// A block takes a chunk of the elements of up to kReadRows rows: base is loaded
+// once for them.
+constexpr int kReadRows = 4;
+constexpr int kReadChunk = kThreads * 4;
+template <int F, bool NT, bool Full>
+__device__ __forceinline__ void dequantize_chunk(const DequantizeParams &p, int32_t k0, int64_t e) {
     using Code = typename Fmt<F>::Code;
-    for (uint32_t b = blockIdx.x; b < p.g.blocks; b += gridDim.x) {
-        uint32_t k, piece;
-        if (!row_piece(p.g, b, &k, &piece)) continue;
-        const int64_t e0 = (int64_t)piece * (kThreads * 4 * NU) + threadIdx.x * 4;
-        uint32_t c[NU], s[NU];
+    const int64_t at = Full || e < p.P ? e : (p.P - 1) / 4 * 4;
+    uint32_t c[kReadRows], s[kReadRows];
+    f4 b = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            const int64_t e = e0 + u * (kThreads * 4);
-            if (e >= p.P) continue;
-            c[u] = *reinterpret_cast<const Code *>(p.codes + k * p.code_ld + (e >> 2) * sizeof(Code));
-            s[u] = p.scales[k * p.scale_ld + (e >> 5)];
-        }
+    for (int i = 0; i < kReadRows; ++i) {
+        if (k0 + i >= p.K) break;
+        c[i] = *reinterpret_cast<const Code *>(p.codes + (k0 + i) * p.code_ld + (at >> 2) * sizeof(Code));
+        s[i] = p.scales[(k0 + i) * p.scale_ld + (at >> 5)];
+    }
+    if (p.base) b = load4<false, Full>(p.base, e, p.P);
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            const int64_t e = e0 + u * (kThreads * 4);
-            if (e >= p.P) continue;
-            f4 v = Fmt<F>::decode(c[u], scale_of(s[u]));
-            if (p.base) v = load4(p.base, e, p.P) + v;
-            store4(p.y + k * p.y_ld, e, p.P, v);
-        }
+    for (int i = 0; i < kReadRows; ++i) {
+        if (k0 + i >= p.K) break;
+        f4 v = Fmt<F>::decode(c[i], scale_of(s[i]));
+        if (p.base) v = b + v;
+        store4<NT, Full>(p.y + (k0 + i) * p.y_ld, e, p.P, v);
+    }
+}
+
+template <int F, bool NT>
+__global__ void __launch_bounds__(kThreads) k_mx_dequantize(DequantizeParams p) {
+    for (uint32_t b = blockIdx.x; b < p.blocks; b += gridDim.x) {
+        // the groups of rows of one chunk follow one another on one XCD
+        const uint32_t s = b / p.spread;
+        const int32_t k0 = (int32_t)(s % p.groups) * kReadRows;
+        const int64_t c0 = (int64_t)(s / p.groups * p.spread + b % p.spread) * kReadChunk;
+        if (c0 >= p.P) continue;
+        if (c0 + kReadChunk <= p.P) dequantize_chunk<F, NT, true>(p, k0, c0 + threadIdx.x * 4);
+        else dequantize_chunk<F, NT, false>(p, k0, c0 + threadIdx.x * 4);
     }
 }
 
@@ -299,24 +331,50 @@ struct AverageParams {
 // the workers, s1 of d and s2 of d^2, are exact unless their scales are 2^40
 // apart, so K s2 - s1^2 = K sum_k (d_k - mean)^2 loses nothing where the
 // workers agree, and one pass over the rows is enough.
-template <int F, int NU>
-__global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
+constexpr int kRowsAtOnce = 8;     // rows whose codes are in flight together
+constexpr int kAverageGroups = 2;  // float4 groups of a lane in a large problem
+
+template <int F, int NU, bool NT, bool Full>
+__device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0, int64_t c1, double s2[NU][4],
+                                              int32_t *tau, double *all) {
     using Code = typename Fmt<F>::Code;
-    __shared__ double lds[kThreads / 64];
-    const double inv = 1.0 / (double)p.K;
-    for (uint32_t c = blockIdx.x; c < p.chunks; c += gridDim.x) {
-        const int64_t c0 = (int64_t)c * (kThreads * 4 * NU);
-        const int64_t c1 = c0 + kThreads * 4 * NU < p.P ? c0 + kThreads * 4 * NU : p.P;
-        const int64_t e0 = c0 + threadIdx.x * 4;
-        double s1[NU][4] = {}, s2[NU][4] = {};
-        for (int32_t k = 0; k < p.K; ++k) {
-            const uint8_t *codes = p.codes + k * p.code_ld, *scales = p.scales + k * p.scale_ld;
+    const int64_t e0 = c0 + threadIdx.x * 4;
+    double s1[NU][4] = {};
+    int64_t at[NU];
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        at[u] = e0 + u * (kThreads * 4);
+        if (!Full && at[u] >= p.P) at[u] = (p.P - 1) / 4 * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s2[u][j] = 0.0;
+    }
+    f4 b[NU];
+    for (int32_t k0 = 0; k0 < p.K; k0 += kRowsAtOnce) {
+        uint32_t c[kRowsAtOnce][NU], s[kRowsAtOnce][NU];
+#pragma unroll
+        for (int i = 0; i < kRowsAtOnce; ++i) {
+            if (k0 + i >= p.K) break;
+            const uint8_t *codes = p.codes + (k0 + i) * p.code_ld, *scales = p.scales + (k0 + i) * p.scale_ld;
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
-                const int64_t e = e0 + u * (kThreads * 4);
-                if (e >= p.P) continue;
-                const f4 v = Fmt<F>::decode(*reinterpret_cast<const Code *>(codes + (e >> 2) * sizeof(Code)),
-                                            scale_of(scales[e >> 5]));
+                c[i][u] = *reinterpret_cast<const Code *>(codes + (at[u] >> 2) * sizeof(Code));
+                s[i][u] = scales[at[u] >> 5];
+            }
+        }
+        if (k0 == 0) {     // the rest that has to come from memory, behind the first rows
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                b[u] = f4{0.f, 0.f, 0.f, 0.f};
+                if (p.base) b[u] = load4<false, Full>(p.base, e0 + u * (kThreads * 4), p.P);
+            }
+            *tau = tensor_at(p.off, p.T, c0);
+        }
+#pragma unroll
+        for (int i = 0; i < kRowsAtOnce; ++i) {
+            if (k0 + i >= p.K) break;
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                const f4 v = Fmt<F>::decode(c[i][u], scale_of(s[i][u]));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const double d = v[j];
@@ -325,26 +383,36 @@ __global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
                 }
             }
         }
-        double all = 0.0;
+    }
+    const double inv = 1.0 / (double)p.K;
+    *all = 0.0;
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            const int64_t e = e0 + u * (kThreads * 4);
-            if (e >= p.P) continue;
-            f4 v = {0.f, 0.f, 0.f, 0.f};
-            if (p.base) v = load4(p.base, e, p.P);
+    for (int u = 0; u < NU; ++u) {
+        const int64_t e = e0 + u * (kThreads * 4);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = (float)((double)v[j] + s1[u][j] * inv);
-                double q = (double)p.K * s2[u][j] - s1[u][j] * s1[u][j];
-                q = e + j < p.P ? (q < 0.0 ? 0.0 : q) : 0.0;    // (a NaN stays)
-                s2[u][j] = q;
-                all += q;
-            }
-            if (p.base_out) store4(p.base_out, e, p.P, v);
-            if (p.x)
-                for (int32_t k = 0; k < p.K; ++k) store4(p.x + k * p.x_ld, e, p.P, v);
+        for (int j = 0; j < 4; ++j) {
+            b[u][j] = (float)((double)b[u][j] + s1[u][j] * inv);
+            double q = (double)p.K * s2[u][j] - s1[u][j] * s1[u][j];
+            q = Full || e + j < c1 ? (q < 0.0 ? 0.0 : q) : 0.0;    // (a NaN stays)
+            s2[u][j] = q;
+            *all += q;
         }
-        int32_t tau = tensor_at(p.off, p.T, c0);
+        if (p.base_out) store4<NT, Full>(p.base_out, e, p.P, b[u]);
+        if (p.x)
+            for (int32_t k = 0; k < p.K; ++k) store4<NT, Full>(p.x + k * p.x_ld, e, p.P, b[u]);
+    }
+}
+
+template <int F, int NU, bool NT>
+__global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
+    __shared__ double lds[kThreads / 64];
+    constexpr int kChunk = kThreads * 4 * NU;
+    for (uint32_t c = blockIdx.x; c < p.chunks; c += gridDim.x) {
+        const int64_t c0 = (int64_t)c * kChunk, c1 = c0 + kChunk < p.P ? c0 + kChunk : p.P;
+        double q[NU][4], all;
+        int32_t tau;
+        if (c0 + kChunk <= p.P) average_chunk<F, NU, NT, true>(p, c0, c1, q, &tau, &all);
+        else average_chunk<F, NU, NT, false>(p, c0, c1, q, &tau, &all);
         if (p.off[tau + 1] >= c1) {
             all = block_sum(all, lds);
             if (threadIdx.x == 0) p.partials[(int64_t)c + tau] = all;
@@ -358,8 +426,8 @@ __global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
             for (int u = 0; u < NU; ++u)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int64_t e = e0 + u * (kThreads * 4) + j;
-                    if (e >= lo && e < hi) part += s2[u][j];
+                    const int64_t e = c0 + threadIdx.x * 4 + u * (kThreads * 4) + j;
+                    if (e >= lo && e < hi) part += q[u][j];
                 }
             part = block_sum(part, lds);
             if (threadIdx.x == 0) p.partials[(int64_t)c + tau] = part;
@@ -368,15 +436,21 @@ __global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
 }
 
 // One block per tensor: the sum of its chunks' partial sums over K^2.
-__global__ void __launch_bounds__(kThreads) k_mx_variance(const int64_t *off, const double *partials, int64_t chunk,
-                                                          int64_t P, int32_t T, double k2, double *var) {
-    __shared__ double lds[kThreads / 64];
+__global__ void __launch_bounds__(1024) k_mx_variance(const int64_t *off, const double *partials, int64_t chunk,
+                                                      int64_t P, int32_t T, double k2, double *var) {
+    __shared__ double lds[16];
     for (int32_t tau = blockIdx.x; tau < T; tau += gridDim.x) {
         const int64_t lo = off[tau] > 0 ? off[tau] : 0, hi = off[tau + 1] < P ? off[tau + 1] : P;
         double s = 0.0;
         if (hi > lo) {
             const int64_t last = (hi - 1) / chunk;
-            for (int64_t c = lo / chunk + threadIdx.x; c <= last; c += kThreads) s += partials[c + tau];
+            // (threads past a short tensor's chunks add nothing)
+            double t[4] = {};
+            int64_t c = lo / chunk + threadIdx.x;
+            for (; c + 3 * (int64_t)blockDim.x <= last; c += 4 * (int64_t)blockDim.x)
+                for (int i = 0; i < 4; ++i) t[i] += partials[c + i * (int64_t)blockDim.x + tau];
+            for (; c <= last; c += blockDim.x) t[0] += partials[c + tau];
+            s = (t[0] + t[1]) + (t[2] + t[3]);
         }
         s = block_sum(s, lds);
         if (threadIdx.x == 0) var[tau] = s / k2;
@@ -394,6 +468,9 @@ __global__ void __launch_bounds__(kThreads) k_mx_variance(const int64_t *off, co
 //   E4M3: the 8-bit instructions drop products 2^-15 below the largest of
 //         their sum, so the codes are converted to bf16, exactly and with
 //         their scales (an element below 2^-126 becomes zero), for the bf16 instruction.
+// Where K <= 8, the 16 rows of the tile are 16 / R stretches of 512 elements of
+// R = 1, 2, 4 or 8 workers: products of different stretches come out too and
+// are left out.
 constexpr int kSuper = 512;
 
 struct ProductParams {
@@ -403,30 +480,21 @@ struct ProductParams {
     int64_t code_ld, scale_ld;    // of a
     int64_t b_code_ld, b_scale_ld;
     int64_t P;
-    int64_t chunk;         // elements, a multiple of 4 kSuper
+    int64_t chunk;         // elements, a multiple of 4 stretches kSuper
     uint32_t chunks;
     int32_t K, T;
+    int32_t R, stretches;  // 16 and 1 where K > 8
 };
 
-// Keep the elements of 16-byte unit [first, first + n) that lie in [lo, hi).
-template <int F>
-__device__ __forceinline__ void mask_unit(u4 &v, uint32_t &scale, int64_t first, int64_t lo, int64_t hi) {
-    constexpr int n = F == ADPSGD_MX_E2M1 ? 32 : 16, bits = 128 / n, per = 32 / bits;
-    int64_t a = lo - first, b = hi - first;
-    a = a < 0 ? 0 : a;
-    b = b > n ? n : b;
-    if (a >= b) {
-        v = u4{0, 0, 0, 0};
-        scale = 127;       // (nothing here is this tensor's, a NaN scale neither)
-        return;
-    }
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        uint32_t m = 0;
-        for (int j = 0; j < per; ++j)
-            if (w * per + j >= a && w * per + j < b) m |= ((bits == 4 ? 0xfu : 0xffu) << (bits * j));
-        v[w] &= m;
-    }
+// Bits of the elements [a, b) of 32 / bits elements from w * (32 / bits) on.
+template <int bits>
+__device__ __forceinline__ uint32_t element_mask(int a, int b, int w) {
+    constexpr int per = 32 / bits;
+    a -= w * per;
+    b -= w * per;
+    a = a < 0 ? 0 : (a > per ? per : a);
+    b = b < 0 ? 0 : (b > per ? per : b);
+    return (uint32_t)((1ull << (bits * b)) - 1) & ~(uint32_t)((1ull << (bits * a)) - 1);
 }
 
 // A unit of E4M3 codes as two operands of the bf16 instruction.
@@ -445,14 +513,7 @@ __device__ __forceinline__ void bf16_of(const u4 &v, uint32_t byte, bf8v *out) {
     }
 }
 
-// One 16-byte unit of NT tiles of 16 rows, and its scale.
-template <int F, int NT>
-struct Unit {
-    u4 code[NT];
-    uint32_t scale[NT];
-};
-
-// Scale bytes of a superblock's units j of this lane, out of the row's 16.
+// The scale byte of this lane's unit j, out of the 16 of its 512 elements.
 template <int F>
 __device__ __forceinline__ uint32_t unit_scale(const u4 &bytes, int j) {
     const int q = (threadIdx.x & 63) >> 4;
@@ -460,18 +521,127 @@ __device__ __forceinline__ uint32_t unit_scale(const u4 &bytes, int j) {
     else return (bytes[j >> 1] >> (16 * (j & 1) + 8 * (q >> 1))) & 0xff;
 }
 
-template <int F>
-__device__ __forceinline__ v4 multiply(const u4 &a, uint32_t sa, const u4 &b, uint32_t sb, v4 acc) {
+// acc += the products of unit a's tiles with unit o's (One: o is a, and the
+// tiles below the diagonal are left out).
+template <int F, int NT, bool One>
+__device__ __forceinline__ void multiply(const u4 *a, const uint32_t *sa, const u4 *o, const uint32_t *so,
+                                         v4 (&acc)[NT][NT]) {
     if constexpr (F == ADPSGD_MX_E2M1) {
-        const i8v x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-        const i8v y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, 0, (int)sa, 0, (int)sb);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const i8v x = {(int)a[i][0], (int)a[i][1], (int)a[i][2], (int)a[i][3], 0, 0, 0, 0};
+#pragma unroll
+            for (int t = One ? i : 0; t < NT; ++t) {
+                const i8v y = {(int)o[t][0], (int)o[t][1], (int)o[t][2], (int)o[t][3], 0, 0, 0, 0};
+                acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc[i][t], 4, 4, 0, (int)sa[i], 0,
+                                                                             (int)so[t]);
+            }
+        }
     } else {
-        bf8v x[2], y[2];
-        bf16_of(a, sa, x);
-        bf16_of(b, sb, y);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[0], y[0], acc, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[1], y[1], acc, 0, 0, 0);
+        bf8v x[NT][2], y[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            bf16_of(a[t], sa[t], x[t]);
+            if (!One) bf16_of(o[t], so[t], y[t]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int t = One ? i : 0; t < NT; ++t)
+                    acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][h], One ? x[t][h] : y[t][h], acc[i][t], 0, 0, 0);
+    }
+}
+
+// One operand's rows as a lane holds them.
+template <int NT>
+struct Lanes {
+    const uint8_t *codes[NT], *scales[NT];
+    __device__ __forceinline__ void point(const uint8_t *c, const uint8_t *s, int64_t code_ld, int64_t scale_ld,
+                                          int32_t row0, int32_t R, int32_t K) {
+        const int r = threadIdx.x & 15;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            // (rows past K repeat the last one: their part of C is not kept)
+            int32_t k = NT == 1 ? row0 + r % R : row0 + t * 16 + r;
+            k = k < K ? k : K - 1;
+            codes[t] = c + k * code_ld;
+            scales[t] = s + k * scale_ld;
+        }
+    }
+};
+
+// The products of 512 elements of each of the tile's rows; stretch: this lane's
+// first element over 512.  Edge: part of them is not in [lo, hi).
+template <int F, int NT, bool One, bool Edge>
+__device__ __forceinline__ void product_super(const Lanes<NT> &A, const Lanes<NT> &B, int64_t stretch, int64_t lo,
+                                              int64_t hi, int64_t P, v4 (&acc)[NT][NT]) {
+    constexpr int kUnits = F == ADPSGD_MX_E2M1 ? 4 : 8;         // a lane's units of 512 elements
+    constexpr int kBits = F == ADPSGD_MX_E2M1 ? 4 : 8, n = 128 / kBits;
+    const int q = (threadIdx.x & 63) >> 4;
+    int64_t st = stretch, last = 0;
+    if (Edge) {      // stay inside the rows: what is read again is masked
+        const int64_t top = (P - 1) / kSuper;
+        st = st < top ? st : top;
+        last = (P + kMxBlock - 1) / kMxBlock * (kMxBlock / n) - 1;
+    }
+    // units in flight together: what the registers hold
+    constexpr int kFly = NT == 1 ? kUnits : NT == 2 ? 4 : 2;
+    u4 sa[NT], sb[NT], a[kFly][NT], b[kFly][NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        sa[t] = *reinterpret_cast<const u4 *>(A.scales[t] + st * 16);
+        if (!One) sb[t] = *reinterpret_cast<const u4 *>(B.scales[t] + st * 16);
+    }
+    int from = 0, to = kSuper;
+    if (Edge) {
+        const int64_t e = stretch * kSuper;
+        from = lo <= e ? 0 : (lo - e < kSuper ? (int)(lo - e) : kSuper);
+        to = hi - e >= kSuper ? kSuper : (hi > e ? (int)(hi - e) : 0);
+    }
+#pragma unroll
+    for (int j0 = 0; j0 < kUnits; j0 += kFly) {
+#pragma unroll
+        for (int j = 0; j < kFly; ++j) {
+            int64_t u = st * (4 * kUnits) + 4 * (j0 + j) + q;
+            if (Edge) u = u < last ? u : last;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                a[j][t] = *reinterpret_cast<const u4 *>(A.codes[t] + u * 16);
+                if (!One) b[j][t] = *reinterpret_cast<const u4 *>(B.codes[t] + u * 16);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kFly; ++j) {
+            uint32_t ba[NT], bb[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                ba[t] = unit_scale<F>(sa[t], j0 + j);
+                if (!One) bb[t] = unit_scale<F>(sb[t], j0 + j);
+            }
+            if (Edge) {
+                const int first = (4 * (j0 + j) + q) * n;
+                const bool none = first >= to || first + n <= from;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t m = none ? 0u : element_mask<kBits>(from - first, to - first, w);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        a[j][t][w] &= m;
+                        if (!One) b[j][t][w] &= m;
+                    }
+                }
+                // (none of this tensor's elements: neither is a NaN scale its own)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    ba[t] = none ? 127u : ba[t];
+                    if (!One) bb[t] = none ? 127u : bb[t];
+                }
+            }
+            multiply<F, NT, One>(a[j], ba, One ? a[j] : b[j], One ? ba : bb, acc);
+        }
+        if (kFly < kUnits) __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -484,11 +654,9 @@ enum { kDiagonal = 0, kAbove = 1, kEvery = 2 };
 template <int F, int NT, int Pairs>
 __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     constexpr bool kOne = Pairs == kDiagonal;
-    constexpr int kUnits = F == ADPSGD_MX_E2M1 ? 4 : 8;   // a lane's units of a superblock
-    constexpr int kUnitElems = F == ADPSGD_MX_E2M1 ? 32 : 16;
-    __shared__ float lds[kThreads / 64][256];
+    constexpr int kWaves = kThreads / 64;
+    __shared__ float lds[kWaves][NT * NT][256];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t units = (p.P + kMxBlock - 1) / kMxBlock * (kMxBlock / kUnitElems);
     const int32_t groups = (p.K + 16 * NT - 1) / (16 * NT);
     int32_t I = blockIdx.y, J = blockIdx.y;
     if (Pairs == kEvery) {
@@ -502,19 +670,12 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
         }
         J += I + 1;
     }
-    // this lane's rows; those past K repeat the last one: their part of C is not kept
-    const uint8_t *ac[NT], *as[NT], *bc[NT], *bs[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        int32_t r = (I * NT + t) * 16 + (lane & 15);
-        r = r < p.K ? r : p.K - 1;
-        ac[t] = p.ac + r * p.code_ld;
-        as[t] = p.as + r * p.scale_ld;
-        r = (J * NT + t) * 16 + (lane & 15);
-        r = r < p.K ? r : p.K - 1;
-        bc[t] = p.bc + r * p.b_code_ld;
-        bs[t] = p.bs + r * p.b_scale_ld;
-    }
+    Lanes<NT> A, B;
+    A.point(p.ac, p.as, p.code_ld, p.scale_ld, I * 16 * NT, p.R, p.K);
+    if (!kOne) B.point(p.bc, p.bs, p.b_code_ld, p.b_scale_ld, J * 16 * NT, p.R, p.K);
+    const int32_t stretches = NT == 1 ? p.stretches : 1;
+    const int32_t mine = NT == 1 ? (lane & 15) / p.R : 0;
+    const int64_t super = (int64_t)stretches * kSuper;
     for (uint32_t c = blockIdx.x; c < p.chunks; c += gridDim.x) {
         const int64_t c0 = (int64_t)c * p.chunk;
         const int64_t c1 = c0 + p.chunk < p.P ? c0 + p.chunk : p.P;
@@ -528,75 +689,77 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
             for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
-            for (int64_t sb = lo / kSuper + wave; sb * kSuper < hi; sb += kThreads / 64) {
-                const bool edge = sb * kSuper < lo || (sb + 1) * kSuper > hi;
-                u4 sa[NT], sbb[NT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    sa[t] = *reinterpret_cast<const u4 *>(as[t] + sb * 16);
-                    if (!kOne) sbb[t] = *reinterpret_cast<const u4 *>(bs[t] + sb * 16);
-                }
-#pragma unroll
-                for (int j = 0; j < kUnits; ++j) {
-                    const int64_t at = sb * (4 * kUnits) + 4 * j + (lane >> 4);
-                    const int64_t u = at < units ? at : units - 1;
-                    Unit<F, NT> a, b;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        a.code[t] = *reinterpret_cast<const u4 *>(ac[t] + u * 16);
-                        a.scale[t] = unit_scale<F>(sa[t], j);
-                        if (!kOne) {
-                            b.code[t] = *reinterpret_cast<const u4 *>(bc[t] + u * 16);
-                            b.scale[t] = unit_scale<F>(sbb[t], j);
-                        }
-                        if (edge) {
-                            mask_unit<F>(a.code[t], a.scale[t], at * kUnitElems, lo, hi);
-                            if (!kOne) mask_unit<F>(b.code[t], b.scale[t], at * kUnitElems, lo, hi);
-                        }
-                    }
-                    const Unit<F, NT> &o = kOne ? a : b;
-#pragma unroll
-                    for (int i = 0; i < NT; ++i)
-#pragma unroll
-                        for (int t = kOne ? i : 0; t < NT; ++t)
-                            acc[i][t] = multiply<F>(a.code[i], a.scale[i], o.code[t], o.scale[t], acc[i][t]);
-                }
+            for (int64_t sb = lo / super + wave; sb * super < hi; sb += kWaves) {
+                const int64_t stretch = sb * stretches + mine;
+                if (sb * super >= lo && (sb + 1) * super <= hi)
+                    product_super<F, NT, kOne, false>(A, B, stretch, lo, hi, p.P, acc);
+                else
+                    product_super<F, NT, kOne, true>(A, B, stretch, lo, hi, p.P, acc);
             }
-            // the four waves' tiles, summed, into the pair's partial sum
-            float *out = p.partials + ((int64_t)c + tau) * p.K * p.K;
+            // the waves' tiles (and the stretches' parts of one), summed, into the pair's partial sum
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int j = kOne ? i : 0; j < NT; ++j) {
+                for (int j = kOne ? i : 0; j < NT; ++j)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) lds[wave][(4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[i][j][r];
-                    __syncthreads();
-                    const int32_t row = (I * NT + i) * 16 + (int32_t)threadIdx.x / 16;
-                    const int32_t col = (J * NT + j) * 16 + (int32_t)threadIdx.x % 16;
+                    for (int r = 0; r < 4; ++r)
+                        lds[wave][i * NT + j][(4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[i][j][r];
+            __syncthreads();
+            float *out = p.partials + ((int64_t)c + tau) * p.K * p.K;
+            const int32_t row = (int32_t)threadIdx.x / 16, col = (int32_t)threadIdx.x % 16;
+            if (NT == 1) {
+                if (I * 16 + row < p.K && J * 16 + col < p.K && row < p.R && col < p.R) {
                     double s = 0.0;
-                    for (int w = 0; w < kThreads / 64; ++w) s += lds[w][threadIdx.x];
-                    if (row < p.K && col < p.K) out[(int64_t)row * p.K + col] = (float)s;
-                    __syncthreads();
+                    for (int w = 0; w < kWaves; ++w)
+                        for (int g = 0; g < stretches; ++g) s += lds[w][0][(g * p.R + row) * 16 + g * p.R + col];
+                    out[row * p.K + col] = (float)s;
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int j = kOne ? i : 0; j < NT; ++j) {
+                        const int32_t y = (I * NT + i) * 16 + row, x = (J * NT + j) * 16 + col;
+                        double s = 0.0;
+                        for (int w = 0; w < kWaves; ++w) s += lds[w][i * NT + j][threadIdx.x];
+                        if (y < p.K && x < p.K) out[(int64_t)y * p.K + x] = (float)s;
+                    }
+            }
+            __syncthreads();
         }
     }
 }
 
-// The tensors' sums of their chunks' partial sums; where b is a, tiles below
-// the diagonal are the transposed ones above it.
-__global__ void __launch_bounds__(kThreads) k_mx_product_sum(const int64_t *off, const float *partials, int64_t chunk,
-                                                             int64_t P, int32_t K, int32_t T, int same, float *out) {
+// The tensors' sums of their chunks' partial sums, in 64 bits, by lanes of
+// `outs` entries: blockDim / outs of them share a tensor's chunks.  Where b is a,
+// tiles below the diagonal are the transposed ones above it.
+__global__ void __launch_bounds__(1024) k_mx_product_sum(const int64_t *off, const float *partials, int64_t chunk,
+                                                         int64_t P, int32_t K, int32_t T, int same, int32_t outs,
+                                                         float *out) {
+    __shared__ double lds[1024];
     const int64_t n = (int64_t)K * K;
+    const int32_t share = blockDim.x / outs, part = threadIdx.x / outs;
+    const int64_t i = (int64_t)blockIdx.y * outs + threadIdx.x % outs;
+    const int32_t row = (int32_t)(i / K), col = (int32_t)(i % K);
+    const float *from = partials + (same && row / 16 > col / 16 ? (int64_t)col * K + row : i);
     for (int32_t tau = blockIdx.x; tau < T; tau += gridDim.x) {
         const int64_t lo = off[tau] > 0 ? off[tau] : 0, hi = off[tau + 1] < P ? off[tau + 1] : P;
-        const int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x;
-        if (i >= n) continue;
-        const int32_t row = (int32_t)(i / K), col = (int32_t)(i % K);
-        const int64_t at = same && row / 16 > col / 16 ? (int64_t)col * K + row : i;
-        double s = 0.0;
-        if (hi > lo)
-            for (int64_t c = lo / chunk; c <= (hi - 1) / chunk; ++c) s += partials[(c + tau) * n + at];
-        out[tau * n + i] = (float)s;
+        double s[4] = {};
+        if (hi > lo && i < n) {
+            const int64_t last = (hi - 1) / chunk;
+            int64_t c = lo / chunk + part;
+            for (; c + 3 * (int64_t)share <= last; c += 4 * (int64_t)share)
+                for (int u = 0; u < 4; ++u) s[u] += from[(c + u * (int64_t)share + tau) * n];
+            for (; c <= last; c += share) s[0] += from[(c + tau) * n];
+        }
+        lds[threadIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
+        __syncthreads();
+        if (part == 0 && i < n) {
+            double t = 0.0;
+            for (int32_t w = 0; w < share; ++w) t += lds[w * outs + threadIdx.x];
+            out[tau * n + i] = (float)t;
+        }
+        __syncthreads();
     }
 }
 
@@ -713,21 +876,24 @@ int launched(const char *what) {
 
 uint32_t grid_for(uint64_t blocks) { return (uint32_t)(blocks < kMaxGrid ? blocks : kMaxGrid); }
 
-// Four groups a lane keep more loads in flight; one spreads a small problem
-// over more of the chip.
-bool four_groups(int64_t elements) { return elements >= int64_t(1) << 22; }
+// fp32 rows beyond the 256 MB last-level cache go past it.
+bool past_cache(int64_t K, int64_t P) { return (double)K * (double)P * 4.0 > 256e6; }
 
-int64_t average_chunk(int64_t P) {
-    return kThreads * 4 * (four_groups(P) ? 4 : 1);
-}
+// Several groups a lane for long rows (half the blocks' fixed work), one where
+// that would leave compute units without a block.
+bool long_rows(int64_t P) { return P >= int64_t(1) << 22; }
 
-// Elements of a product block: 2048 blocks of whole superblocks for each wave,
-// at most 16384 elements (of which fp32 sums are taken) for one wave.
-int64_t product_chunk(int64_t P) {
-    const int64_t step = 4 * kSuper;
-    int64_t n = (P / 2048 + step - 1) / step * step;
-    n = n < step ? step : n;
-    return n > 65536 ? 65536 : n;
+int64_t average_chunk_elements(int64_t P) { return kThreads * 4 * (long_rows(P) ? kAverageGroups : 1); }
+
+// Workers of a tile where several stretches share it.
+int32_t tile_workers(int32_t K) { return K > 8 ? 16 : K > 4 ? 8 : K > 2 ? 4 : K; }
+
+// Elements of a product block: 2048 blocks of a whole tile for each wave, at
+// most 16384 elements (of which fp32 sums are taken) for one wave.
+int64_t product_chunk(int32_t K, int64_t P) {
+    const int64_t step = 4 * kSuper * (16 / tile_workers(K));
+    const int64_t n = (P / 2048 + step - 1) / step * step;
+    return n < step ? step : n > 65536 ? 65536 : n;
 }
 
 }  // namespace
@@ -773,19 +939,44 @@ extern "C" int adpsgd_mx_quantize(const adpsgd_mx_rows *out, const float *x, int
     p.code_ld = out->code_stride;
     p.scale_ld = out->scale_stride;
     p.P = P;
-    const bool four = four_groups(out->K * P);
-    p.g = row_grid(out->K, P, kThreads * 4 * (four ? 4 : 1));
-    const dim3 grid(grid_for(p.g.blocks)), block(kThreads);
+    p.g = row_grid(out->K, P, 1);
+    const dim3 grid(grid_for(p.g.blocks)), block(64);
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool nt = past_cache(out->K, P);
     if (out->format == ADPSGD_MX_E2M1) {
-        if (four) k_mx_quantize<ADPSGD_MX_E2M1, 4><<<grid, block, 0, st>>>(p);
-        else k_mx_quantize<ADPSGD_MX_E2M1, 1><<<grid, block, 0, st>>>(p);
+        if (nt) k_mx_quantize<ADPSGD_MX_E2M1, true><<<grid, block, 0, st>>>(p);
+        else k_mx_quantize<ADPSGD_MX_E2M1, false><<<grid, block, 0, st>>>(p);
     } else {
-        if (four) k_mx_quantize<ADPSGD_MX_E4M3, 4><<<grid, block, 0, st>>>(p);
-        else k_mx_quantize<ADPSGD_MX_E4M3, 1><<<grid, block, 0, st>>>(p);
+        if (nt) k_mx_quantize<ADPSGD_MX_E4M3, true><<<grid, block, 0, st>>>(p);
+        else k_mx_quantize<ADPSGD_MX_E4M3, false><<<grid, block, 0, st>>>(p);
     }
     return launched("quantize launch");
 }
+
+namespace {
+
+template <int F>
+void launch_dequantize(DequantizeParams &p, int32_t K, hipStream_t st) {
+    p.K = K;
+    p.groups = (uint32_t)((K + kReadRows - 1) / kReadRows);
+    const uint32_t chunks = (uint32_t)((p.P + kReadChunk - 1) / kReadChunk);
+    p.spread = chunks >= 8 ? 8 : 1;
+    p.blocks = (chunks + p.spread - 1) / p.spread * p.spread * p.groups;
+    if (past_cache(K, p.P)) k_mx_dequantize<F, true><<<grid_for(p.blocks), kThreads, 0, st>>>(p);
+    else k_mx_dequantize<F, false><<<grid_for(p.blocks), kThreads, 0, st>>>(p);
+}
+
+template <int F>
+void launch_average(const AverageParams &p, hipStream_t st) {
+    const bool nt = past_cache(p.K, p.P), several = long_rows(p.P);
+    const uint32_t grid = grid_for(p.chunks);
+    if (several && nt) k_mx_average<F, kAverageGroups, true><<<grid, kThreads, 0, st>>>(p);
+    else if (several) k_mx_average<F, kAverageGroups, false><<<grid, kThreads, 0, st>>>(p);
+    else if (nt) k_mx_average<F, 1, true><<<grid, kThreads, 0, st>>>(p);
+    else k_mx_average<F, 1, false><<<grid, kThreads, 0, st>>>(p);
+}
+
+}  // namespace
 
 extern "C" int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *base, float *y, int64_t y_stride,
                                     void *stream) {
@@ -806,23 +997,15 @@ extern "C" int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *bas
     p.code_ld = rows->code_stride;
     p.scale_ld = rows->scale_stride;
     p.P = P;
-    const bool four = four_groups(rows->K * P);
-    p.g = row_grid(rows->K, P, kThreads * 4 * (four ? 4 : 1));
-    const dim3 grid(grid_for(p.g.blocks)), block(kThreads);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (rows->format == ADPSGD_MX_E2M1) {
-        if (four) k_mx_dequantize<ADPSGD_MX_E2M1, 4><<<grid, block, 0, st>>>(p);
-        else k_mx_dequantize<ADPSGD_MX_E2M1, 1><<<grid, block, 0, st>>>(p);
-    } else {
-        if (four) k_mx_dequantize<ADPSGD_MX_E4M3, 4><<<grid, block, 0, st>>>(p);
-        else k_mx_dequantize<ADPSGD_MX_E4M3, 1><<<grid, block, 0, st>>>(p);
-    }
+    if (rows->format == ADPSGD_MX_E2M1) launch_dequantize<ADPSGD_MX_E2M1>(p, rows->K, st);
+    else launch_dequantize<ADPSGD_MX_E4M3>(p, rows->K, st);
     return launched("dequantize launch");
 }
 
 extern "C" size_t adpsgd_mx_average_workspace(int32_t K, int64_t P, int32_t T) {
     if (K < 1 || K > kMaxK || P < 0 || (P + 3) / 4 > (int64_t(1) << 32) || T < 1 || T > kMaxT) return 0;
-    const int64_t chunk = average_chunk(P);
+    const int64_t chunk = average_chunk_elements(P);
     return sizeof(double) * (size_t)((P + chunk - 1) / chunk + T);
 }
 
@@ -857,30 +1040,24 @@ extern "C" int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
     p.code_ld = rows->code_stride;
     p.scale_ld = rows->scale_stride;
     p.P = P;
-    const int64_t chunk = average_chunk(P);
+    const int64_t chunk = average_chunk_elements(P);
     p.chunks = (uint32_t)((P + chunk - 1) / chunk);
     p.K = rows->K;
     p.T = T;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (P > 0) {
-        const dim3 grid(grid_for(p.chunks)), block(kThreads);
-        if (rows->format == ADPSGD_MX_E2M1) {
-            if (four_groups(P)) k_mx_average<ADPSGD_MX_E2M1, 4><<<grid, block, 0, st>>>(p);
-            else k_mx_average<ADPSGD_MX_E2M1, 1><<<grid, block, 0, st>>>(p);
-        } else {
-            if (four_groups(P)) k_mx_average<ADPSGD_MX_E4M3, 4><<<grid, block, 0, st>>>(p);
-            else k_mx_average<ADPSGD_MX_E4M3, 1><<<grid, block, 0, st>>>(p);
-        }
+        if (rows->format == ADPSGD_MX_E2M1) launch_average<ADPSGD_MX_E2M1>(p, st);
+        else launch_average<ADPSGD_MX_E4M3>(p, st);
         if (int rc = launched("average launch")) return rc;
     }
-    k_mx_variance<<<grid_for((uint64_t)T), kThreads, 0, st>>>(tensor_offsets, p.partials, chunk, P, T,
+    k_mx_variance<<<grid_for((uint64_t)T), p.chunks > 4096 ? 1024 : kThreads, 0, st>>>(tensor_offsets, p.partials, chunk, P, T,
                                                               (double)rows->K * rows->K, var);
     return launched("variance launch");
 }
 
 extern "C" size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T) {
     if (K < 1 || K > kMaxProductK || P < 0 || (P + 3) / 4 > (int64_t(1) << 32) || T < 1 || T > kMaxT) return 0;
-    const int64_t chunk = product_chunk(P);
+    const int64_t chunk = product_chunk(K, P);
     return sizeof(float) * (size_t)((P + chunk - 1) / chunk + T) * K * K;
 }
 
@@ -938,18 +1115,24 @@ extern "C" int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *
     p.b_code_ld = b->code_stride;
     p.b_scale_ld = b->scale_stride;
     p.P = P;
-    p.chunk = product_chunk(P);
+    p.chunk = product_chunk(a->K, P);
     p.chunks = (uint32_t)((P + p.chunk - 1) / p.chunk);
     p.K = a->K;
     p.T = T;
+    p.R = tile_workers(a->K);
+    p.stretches = 16 / p.R;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (P > 0) {
         if (a->format == ADPSGD_MX_E2M1) launch_product<ADPSGD_MX_E2M1>(p, same, st);
         else launch_product<ADPSGD_MX_E4M3>(p, same, st);
         if (int rc = launched("product launch")) return rc;
     }
-    const uint32_t per = (uint32_t)(((int64_t)a->K * a->K + kThreads - 1) / kThreads);
-    k_mx_product_sum<<<dim3(grid_for((uint64_t)T), per), kThreads, 0, st>>>(tensor_offsets, p.partials, p.chunk, P,
-                                                                            a->K, T, same, out);
+    // a block for each tensor and 64 entries; many threads to an entry where a tensor may have many chunks
+    const int64_t n = (int64_t)a->K * a->K;
+    int32_t outs = 1;
+    while (outs < 64 && outs < n) outs *= 2;
+    const uint32_t threads = (int64_t)p.chunks > 8 * (int64_t)T ? 1024 : kThreads;
+    k_mx_product_sum<<<dim3(grid_for((uint64_t)T), (uint32_t)((n + outs - 1) / outs)), threads, 0, st>>>(
+        tensor_offsets, p.partials, p.chunk, P, a->K, T, same, outs, out);
     return launched("product sum launch");
 }
