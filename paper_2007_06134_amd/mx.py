@@ -16,32 +16,48 @@ import torch
 
 from ._native import MX_E2M1, MX_E4M3, _check, adpsgd_mx_rows, lib
 
-BLOCK = 32                            # elements that share a scale
+BLOCK = 32                                # elements that share a scale
 _ROW_BYTES = {MX_E2M1: 16, MX_E4M3: 32}   # of codes, a block
+
+# The smallest calls take a few microseconds on the GPU, so the checks below are
+# made of the cheapest queries of a tensor (a device is its index, -1 off the GPU).
+_U8, _F32, _F64, _I64 = torch.uint8, torch.float32, torch.float64, torch.int64
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _run(fn, dev: int, *args) -> None:
+    """fn(*args, current stream) of device dev, made the current device for it."""
+    if _current_device() == dev:
+        rc = fn(*args, _current_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _current_stream(dev))
+    if rc:
+        _check(rc)
 
 
 class MxRows:
     """K rows of P elements: codes [K, >= ceil(P / 32) * 16 (E2M1) or * 32 (E4M3)] and scales
     [K, >= ceil(P / 32)], uint8, rows at strides that are multiples of 16 bytes."""
 
-    __slots__ = ("codes", "scales", "P", "format", "K", "_c")
+    __slots__ = ("codes", "scales", "P", "format", "K", "_dev", "_c", "_ref")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, P: int, format: int = MX_E2M1):
-        if format not in _ROW_BYTES:
+        per = _ROW_BYTES.get(format)
+        if per is None:
             raise ValueError("format must be MX_E2M1 or MX_E4M3")
         if P < 0:
             raise ValueError("P must be >= 0")
         n = -(-P // BLOCK)
-        for t, need, name in ((codes, n * _ROW_BYTES[format], "codes"), (scales, n, "scales")):
-            if t.dtype != torch.uint8 or t.dim() != 2 or t.device.type != "cuda":
-                raise ValueError(f"{name} must be a uint8 matrix on a GPU")
-            if t.shape[1] < need or (t.shape[1] > 1 and t.stride(1) != 1):
-                raise ValueError(f"{name} must have rows of at least {need} contiguous bytes")
-        if codes.shape[0] != scales.shape[0] or codes.device != scales.device:
+        K, code_ld = _bytes(codes, n * per, "codes")
+        K2, scale_ld = _bytes(scales, n, "scales")
+        dev = codes.get_device()
+        if K != K2 or scales.get_device() != dev:
             raise ValueError("codes and scales must have one row a worker on one device")
-        self.codes, self.scales, self.P, self.format, self.K = codes, scales, P, format, codes.shape[0]
-        self._c = adpsgd_mx_rows(codes.data_ptr(), scales.data_ptr(), _row_stride(codes, 16), _row_stride(scales, 16),
-                                 P, self.K, format)
+        self.codes, self.scales, self.P, self.format, self.K, self._dev = codes, scales, P, format, K, dev
+        self._c = adpsgd_mx_rows(codes.data_ptr(), scales.data_ptr(), code_ld, scale_ld, P, K, format)
+        self._ref = C.byref(self._c)
 
     @classmethod
     def empty(cls, K: int, P: int, format: int = MX_E2M1, device="cuda") -> "MxRows":
@@ -50,61 +66,51 @@ class MxRows:
             raise ValueError("format must be MX_E2M1 or MX_E4M3")
         if K < 1 or P < 0:
             raise ValueError("K must be >= 1 and P >= 0")
-        opt = dict(dtype=torch.uint8, device=device)
-        return cls(torch.empty((K, lib.adpsgd_mx_code_stride(format, P)), **opt),
-                   torch.empty((K, lib.adpsgd_mx_scale_stride(P)), **opt), P, format)
+        return cls(torch.empty((K, lib.adpsgd_mx_code_stride(format, P)), dtype=_U8, device=device),
+                   torch.empty((K, lib.adpsgd_mx_scale_stride(P)), dtype=_U8, device=device), P, format)
 
     @property
     def device(self) -> torch.device:
         return self.codes.device
 
 
-def _row_stride(t: torch.Tensor, unit: int) -> int:
-    """Distance of rows; of a single row or empty ones, whose stride means nothing, their length in whole units."""
-    return t.stride(0) if t.shape[0] > 1 and t.shape[1] > 0 else -(-t.shape[1] // unit) * unit
+def _bytes(t: torch.Tensor, need: int, name: str) -> Tuple[int, int]:
+    """Rows of a byte matrix and their distance; of a single row or empty ones, whose stride means
+    nothing, their length in whole units of 16."""
+    if t.dtype is not _U8 or t.dim() != 2 or t.get_device() < 0:
+        raise ValueError(f"{name} must be a uint8 matrix on a GPU")
+    K, w = t.shape
+    if w < need or (w > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must have rows of at least {need} contiguous bytes")
+    return K, t.stride(0) if K > 1 and w > 0 else -(-w // 16) * 16
 
 
-def _matrix(t: torch.Tensor, K: int, P: int, device, name: str) -> int:
+def _matrix(t: torch.Tensor, K: int, P: int, dev: int, name: str) -> int:
     """Row stride of a float32 [K, P] tensor."""
-    if t.dtype != torch.float32 or t.shape != (K, P) or t.device != device:
-        raise ValueError(f"{name} must be float32 [{K}, {P}] on {device}")
+    if t.dtype is not _F32 or t.shape != (K, P) or t.get_device() != dev:
+        raise ValueError(f"{name} must be float32 [{K}, {P}] on device {dev}")
     if P > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    if K > 1 and t.stride(0) < P:
+    if K == 1:
+        return P
+    ld = t.stride(0)
+    if ld < P:
         raise ValueError(f"{name} must have rows that do not overlap")
-    return t.stride(0) if K > 1 else P
+    return ld
 
 
-def _vector(t: Optional[torch.Tensor], P: int, device, name: str) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], P: int, dev: int, name: str) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.shape != (P,) or t.device != device or (P > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be contiguous float32 [{P}] on {device}")
+    if t.dtype is not _F32 or t.shape != (P,) or t.get_device() != dev or (P > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be contiguous float32 [{P}] on device {dev}")
     return t.data_ptr()
 
 
-def _offsets(t: torch.Tensor, device) -> int:
-    if t.dtype != torch.int64 or t.dim() != 1 or t.shape[0] < 2 or t.device != device or t.stride(0) != 1:
-        raise ValueError(f"offsets must be contiguous int64 [T + 1] on {device}")
+def _offsets(t: torch.Tensor, dev: int) -> int:
+    if t.dtype is not _I64 or t.dim() != 1 or t.shape[0] < 2 or t.get_device() != dev or t.stride(0) != 1:
+        raise ValueError(f"offsets must be contiguous int64 [T + 1] on device {dev}")
     return t.shape[0] - 1
-
-
-class _On:
-    """The device of a call made current, and its current stream."""
-
-    __slots__ = ("guard",)
-
-    def __init__(self, device):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
 
 
 def mx_quantize(x: torch.Tensor, base: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, *,
@@ -115,41 +121,40 @@ def mx_quantize(x: torch.Tensor, base: Optional[torch.Tensor] = None, residual: 
     base [P] and residual [K, P] count as zero where they are None.  What the message leaves out is
     written to residual_out, by default to residual itself, and not kept where both are None.
     out: rows to write (their format is the one used)."""
-    if x.dim() != 2 or x.device.type != "cuda":
+    dev = x.get_device()
+    if x.dim() != 2 or dev < 0:
         raise ValueError("x must be a float32 matrix on a GPU")
     K, P = x.shape
-    device = x.device
-    x_ld = _matrix(x, K, P, device, "x")
-    base_ptr = _vector(base, P, device, "base")
-    if residual_out is None:
-        residual_out = residual
+    x_ld = _matrix(x, K, P, dev, "x")
+    base_ptr = _vector(base, P, dev, "base")
     r_in = r_out = None
     r_ld = 0
-    if residual_out is not None:
-        r_ld, r_out = _matrix(residual_out, K, P, device, "residual_out"), residual_out.data_ptr()
     if residual is not None:
-        if _matrix(residual, K, P, device, "residual") != r_ld:
+        r_ld, r_in = _matrix(residual, K, P, dev, "residual"), residual.data_ptr()
+        if residual_out is None:
+            r_out = r_in
+    if residual_out is not None:
+        ld, r_out = _matrix(residual_out, K, P, dev, "residual_out"), residual_out.data_ptr()
+        if residual is not None and ld != r_ld:
             raise ValueError("residual and residual_out must have the same row stride")
-        r_in = residual.data_ptr()
+        r_ld = ld
     if out is None:
-        out = MxRows.empty(K, P, MX_E2M1 if format is None else format, device)
-    elif out.K != K or out.P != P or out.device != device or (format is not None and format != out.format):
-        raise ValueError(f"out must be rows of the format for [{K}, {P}] on {device}")
-    with _On(device) as stream:
-        _check(lib.adpsgd_mx_quantize(C.byref(out._c), x.data_ptr(), x_ld, base_ptr, r_in, r_out, r_ld, stream))
+        out = MxRows.empty(K, P, MX_E2M1 if format is None else format, x.device)
+    elif out.K != K or out.P != P or out._dev != dev or (format is not None and format != out.format):
+        raise ValueError(f"out must be rows of the format for [{K}, {P}] on device {dev}")
+    _run(lib.adpsgd_mx_quantize, dev, out._ref, x.data_ptr(), x_ld, base_ptr, r_in, r_out, r_ld)
     return out
 
 
 def mx_dequantize(rows: MxRows, base: Optional[torch.Tensor] = None, *,
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """What the rows say: base + their values, float32 [K, P]."""
-    device = rows.device
-    base_ptr = _vector(base, rows.P, device, "base")
+    dev = rows._dev
+    base_ptr = _vector(base, rows.P, dev, "base")
     if out is None:
-        out = torch.empty((rows.K, rows.P), dtype=torch.float32, device=device)
-    ld = _matrix(out, rows.K, rows.P, device, "out")
-    with _On(device) as stream:
-        _check(lib.adpsgd_mx_dequantize(C.byref(rows._c), base_ptr, out.data_ptr(), ld, stream))
+        out = torch.empty((rows.K, rows.P), dtype=_F32, device=rows.device)
+    ld = _matrix(out, rows.K, rows.P, dev, "out")
+    _run(lib.adpsgd_mx_dequantize, dev, rows._ref, base_ptr, out.data_ptr(), ld)
     return out
 
 
@@ -161,35 +166,33 @@ def mx_average(rows: MxRows, offsets: torch.Tensor, base: Optional[torch.Tensor]
     offsets: int64 [T + 1] on the device, the tensors' boundaries as for ``Adpsgd`` (0 first, P last;
     the values are not checked).  The new model is also written to every row of x [K, P] where that is
     given, and to base_out (which may be base; a new tensor by default)."""
-    device = rows.device
-    T = _offsets(offsets, device)
-    base_ptr = _vector(base, rows.P, device, "base")
+    dev, K, P = rows._dev, rows.K, rows.P
+    T = _offsets(offsets, dev)
+    base_ptr = _vector(base, P, dev, "base")
     x_ptr, x_ld = None, 0
     if x is not None:
-        x_ld, x_ptr = _matrix(x, rows.K, rows.P, device, "x"), x.data_ptr()
+        x_ld, x_ptr = _matrix(x, K, P, dev, "x"), x.data_ptr()
     if base_out is None:
-        base_out = torch.empty((rows.P,), dtype=torch.float32, device=device)
-    out_ptr = _vector(base_out, rows.P, device, "base_out")
-    var = torch.empty((T,), dtype=torch.float64, device=device)
-    need = lib.adpsgd_mx_average_workspace(rows.K, rows.P, T)
-    work = torch.empty((need,), dtype=torch.uint8, device=device)
-    with _On(device) as stream:
-        _check(lib.adpsgd_mx_average(C.byref(rows._c), T, offsets.data_ptr(), base_ptr, out_ptr, x_ptr, x_ld,
-                                     var.data_ptr(), work.data_ptr(), need, stream))
+        base_out = torch.empty((P,), dtype=_F32, device=rows.device)
+    out_ptr = _vector(base_out, P, dev, "base_out")
+    var = torch.empty((T,), dtype=_F64, device=offsets.device)
+    need = lib.adpsgd_mx_average_workspace(K, P, T)
+    work = torch.empty((need,), dtype=_U8, device=offsets.device)
+    _run(lib.adpsgd_mx_average, dev, rows._ref, T, offsets.data_ptr(), base_ptr, out_ptr, x_ptr, x_ld, var.data_ptr(),
+         work.data_ptr(), need)
     return base_out, var
 
 
 def mx_product(a: MxRows, offsets: torch.Tensor, b: Optional[MxRows] = None) -> torch.Tensor:
     """Inner products of the rows of a with those of b (of a, where b is None) for every tensor:
     float32 [T, K, K].  K is at most 256; a and b have the same format, K and P."""
-    device = a.device
-    T = _offsets(offsets, device)
-    if b is not None and b.device != device:
+    dev, K = a._dev, a.K
+    T = _offsets(offsets, dev)
+    if b is not None and b._dev != dev:
         raise ValueError("a and b must be on one device")
-    out = torch.empty((T, a.K, a.K), dtype=torch.float32, device=device)
-    need = lib.adpsgd_mx_product_workspace(a.K, a.P, T)
-    work = torch.empty((need,), dtype=torch.uint8, device=device)
-    with _On(device) as stream:
-        _check(lib.adpsgd_mx_product(C.byref(a._c), None if b is None else C.byref(b._c), T, offsets.data_ptr(),
-                                     out.data_ptr(), work.data_ptr(), need, stream))
+    out = torch.empty((T, K, K), dtype=_F32, device=offsets.device)
+    need = lib.adpsgd_mx_product_workspace(K, a.P, T)
+    work = torch.empty((need,), dtype=_U8, device=offsets.device)
+    _run(lib.adpsgd_mx_product, dev, a._ref, None if b is None else b._ref, T, offsets.data_ptr(), out.data_ptr(),
+         work.data_ptr(), need)
     return out
