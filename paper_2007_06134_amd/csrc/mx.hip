@@ -17,6 +17,7 @@
 // a table: no plan has to be built before a call.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <initializer_list>
 #include <string>
@@ -124,7 +125,14 @@ __device__ __forceinline__ int32_t tensor_at(const int64_t *off, int32_t T, int6
         lo += at;
         n = n - at < step ? n - at : step;
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Lane i's value, in scalar registers (i the same in all lanes).
+__device__ __forceinline__ int64_t lane_value(int64_t v, int i) {
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
+    const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)v >> 32), i);
+    return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
 // A sum over the block's threads, in the same order every time; valid in thread 0.
@@ -274,7 +282,7 @@ struct DequantizeParams {
 };
 
 // A block takes a chunk of the elements of up to kReadRows rows: base is loaded
-// once for them.
+// once for them (K = 8, P = 138M: 1003 us; 1240 us with a row at a time).
 constexpr int kReadRows = 4;
 constexpr int kReadChunk = kThreads * 4;
 template <int F, bool NT, bool Full>
@@ -435,6 +443,10 @@ __global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
     }
 }
 
+// Partial sums that a thread has on the way at once: few threads share a tensor's,
+// and waiting for each would take longer than reading them.
+constexpr int kBatch = 16;
+
 // One block per tensor: the sum of its chunks' partial sums over K^2.
 __global__ void __launch_bounds__(1024) k_mx_variance(const int64_t *off, const double *partials, int64_t chunk,
                                                       int64_t P, int32_t T, double k2, double *var) {
@@ -444,13 +456,16 @@ __global__ void __launch_bounds__(1024) k_mx_variance(const int64_t *off, const 
         double s = 0.0;
         if (hi > lo) {
             const int64_t last = (hi - 1) / chunk;
-            // (threads past a short tensor's chunks add nothing)
-            double t[4] = {};
-            int64_t c = lo / chunk + threadIdx.x;
-            for (; c + 3 * (int64_t)blockDim.x <= last; c += 4 * (int64_t)blockDim.x)
-                for (int i = 0; i < 4; ++i) t[i] += partials[c + i * (int64_t)blockDim.x + tau];
-            for (; c <= last; c += blockDim.x) t[0] += partials[c + tau];
-            s = (t[0] + t[1]) + (t[2] + t[3]);
+            for (int64_t c = lo / chunk + threadIdx.x; c <= last; c += kBatch * (int64_t)blockDim.x) {
+                double v[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {     // (loads without branches; past the end c's again)
+                    const int64_t at = c + i * (int64_t)blockDim.x;
+                    v[i] = partials[(at <= last ? at : c) + tau];
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) s += c + i * (int64_t)blockDim.x <= last ? v[i] : 0.0;
+            }
         }
         s = block_sum(s, lds);
         if (threadIdx.x == 0) var[tau] = s / k2;
@@ -459,29 +474,34 @@ __global__ void __launch_bounds__(1024) k_mx_variance(const int64_t *off, const 
 
 // ---- product ----------------------------------------------------------------
 // Rows of the two operands are the rows and columns of C, the elements are the
-// contraction, on 16x16 tiles.  A lane holds one row (lane mod 16) and, of
-// every 512 elements, each fourth 16-byte unit (lane / 16).  Which elements
-// share a matrix instruction does not matter to the sum, only that both
-// operands agree.
-//   E2M1: a unit is a block; the scaled 16x16x128 instruction multiplies the
-//         codes and applies both scales; its sums are rounded as fp32.
-//   E4M3: the 8-bit instructions drop products 2^-15 below the largest of
+// contraction, on 16x16 tiles.  Which elements share a matrix instruction does
+// not matter to the sum, only that both operands agree.
+//   E2M1: a 16-byte unit is a block; the scaled 16x16x128 instruction multiplies
+//         the codes and applies both scales; its sums are rounded as fp32.
+//   E4M3: the 8-bit instructions drop products 2^-13 below the largest of
 //         their sum, so the codes are converted to bf16, exactly and with
 //         their scales (an element below 2^-126 becomes zero), for the bf16 instruction.
-// Where K <= 8, the 16 rows of the tile are 16 / R stretches of 512 elements of
-// R = 1, 2, 4 or 8 workers: products of different stretches come out too and
-// are left out.
+// A lane of these instructions holds one row (lane mod 16), but lanes that load
+// 16 bytes of a row each cost an access of the vector cache each, and that many
+// accesses, not memory, set the time (K = 8, P = 138M: 43 million accesses,
+// 117 us).  So four lanes load 64 consecutive bytes of a row, and the units change
+// lanes through the wave's own part of LDS (units of a row rotated by the row
+// over 4, so that neither side meets bank conflicts).
+// Where K <= 8, the 16 rows of the tile are 16 / R stretches of R = 1, 2, 4 or 8
+// workers: products of different stretches come out too and are left out.
 constexpr int kSuper = 512;
+constexpr int kProductWaves = kThreads / 64;
 
 struct ProductParams {
     const uint8_t *ac, *as, *bc, *bs;
     const int64_t *off;
     float *partials;       // [chunks + T][K][K]
+    float *out;            // [T][K][K]
     int64_t code_ld, scale_ld;    // of a
     int64_t b_code_ld, b_scale_ld;
     int64_t P;
-    int64_t chunk;         // elements, a multiple of 4 stretches kSuper
-    uint32_t chunks;
+    int64_t chunk;         // a wave's elements, a multiple of stretches kSuper
+    uint32_t blocks;       // of kProductWaves chunks
     int32_t K, T;
     int32_t R, stretches;  // 16 and 1 where K > 8
 };
@@ -511,14 +531,6 @@ __device__ __forceinline__ void bf16_of(const u4 &v, uint32_t byte, bf8v *out) {
         }
         out[h] = __builtin_bit_cast(bf8v, o);
     }
-}
-
-// The scale byte of this lane's unit j, out of the 16 of its 512 elements.
-template <int F>
-__device__ __forceinline__ uint32_t unit_scale(const u4 &bytes, int j) {
-    const int q = (threadIdx.x & 63) >> 4;
-    if constexpr (F == ADPSGD_MX_E2M1) return (bytes[j] >> (8 * q)) & 0xff;
-    else return (bytes[j >> 1] >> (16 * (j & 1) + 8 * (q >> 1))) & 0xff;
 }
 
 // acc += the products of unit a's tiles with unit o's (One: o is a, and the
@@ -554,109 +566,133 @@ __device__ __forceinline__ void multiply(const u4 *a, const uint32_t *sa, const 
     }
 }
 
-// One operand's rows as a lane holds them.
-template <int NT>
-struct Lanes {
+// 256 bytes of codes, kElems elements, of each row of a wave's tiles in LDS.
+template <int TILES>
+struct WaveLds {
+    u4 code[TILES][4][64];
+    uint32_t scale[TILES][64];
+};
+
+// The loads of a wave: lane l takes row l / 4 of each tile.
+template <int F, int NT>
+struct Fetch {
+    static constexpr int kElems = F == ADPSGD_MX_E2M1 ? 512 : 256;
+    static constexpr int kScaleBytes = kElems / 128;      // a lane's part of a row's kElems / 32
     const uint8_t *codes[NT], *scales[NT];
+    u4 code[NT][4];
+    uint32_t scale[NT];
+
     __device__ __forceinline__ void point(const uint8_t *c, const uint8_t *s, int64_t code_ld, int64_t scale_ld,
                                           int32_t row0, int32_t R, int32_t K) {
-        const int r = threadIdx.x & 15;
+        const int lane = threadIdx.x & 63, r = lane >> 2;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             // (rows past K repeat the last one: their part of C is not kept)
             int32_t k = NT == 1 ? row0 + r % R : row0 + t * 16 + r;
             k = k < K ? k : K - 1;
-            codes[t] = c + k * code_ld;
-            scales[t] = s + k * scale_ld;
+            codes[t] = c + k * code_ld + ((lane & 3) ^ (lane >> 4)) * 16;
+            scales[t] = s + k * scale_ld + (lane & 3) * kScaleBytes;
+        }
+    }
+    // stretch: the lane's row's first element over kElems.  Inside: they all exist;
+    // else units past the row's end are loaded from inside it (and masked later).
+    template <bool Inside>
+    __device__ __forceinline__ void load(int64_t stretch, int64_t P) {
+        const int lane = threadIdx.x & 63;
+        int64_t st = stretch, last = 0;
+        if (!Inside) {
+            const int64_t top = (P - 1) / kElems;
+            st = st < top ? st : top;
+            last = (P + kMxBlock - 1) / kMxBlock * (512 / kElems) - 1 - st * 16 - ((lane & 3) ^ (lane >> 4));
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if constexpr (kScaleBytes == 4) scale[t] = *reinterpret_cast<const uint32_t *>(scales[t] + st * 16);
+            else scale[t] = *reinterpret_cast<const uint16_t *>(scales[t] + st * 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                int64_t u = 4 * j;
+                if (!Inside) u = u < last ? u : last;
+                code[t][j] = *reinterpret_cast<const u4 *>(codes[t] + st * 256 + u * 16);
+            }
+        }
+    }
+    template <int TILES>
+    __device__ __forceinline__ void stash(WaveLds<TILES> &to, int tile0) const {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to.code[tile0 + t][j][lane] = code[t][j];
+            to.scale[tile0 + t][lane] = scale[t];
         }
     }
 };
 
-// The products of 512 elements of each of the tile's rows; stretch: this lane's
-// first element over 512.  Edge: part of them is not in [lo, hi).
-template <int F, int NT, bool One, bool Edge>
-__device__ __forceinline__ void product_super(const Lanes<NT> &A, const Lanes<NT> &B, int64_t stretch, int64_t lo,
-                                              int64_t hi, int64_t P, v4 (&acc)[NT][NT]) {
-    constexpr int kUnits = F == ADPSGD_MX_E2M1 ? 4 : 8;         // a lane's units of 512 elements
+// acc += the products of the elements [from, to) of the rows' kElems (Masked) or of
+// all.  Lane (row r = lane mod 16, q = lane / 16) takes unit 4 q + j of its row in
+// step j.  Uniform: from and to are the same in all lanes.
+template <int F, int NT, bool One, bool Masked, bool Uniform>
+__device__ __forceinline__ void multiply_super(const WaveLds<One ? NT : 2 * NT> &w, int from, int to,
+                                               v4 (&acc)[NT][NT]) {
+    constexpr int TILES = One ? NT : 2 * NT;
     constexpr int kBits = F == ADPSGD_MX_E2M1 ? 4 : 8, n = 128 / kBits;
-    const int q = (threadIdx.x & 63) >> 4;
-    int64_t st = stretch, last = 0;
-    if (Edge) {      // stay inside the rows: what is read again is masked
-        const int64_t top = (P - 1) / kSuper;
-        st = st < top ? st : top;
-        last = (P + kMxBlock - 1) / kMxBlock * (kMxBlock / n) - 1;
-    }
-    // units in flight together: what the registers hold
-    constexpr int kFly = NT == 1 ? kUnits : NT == 2 ? 4 : 2;
-    u4 sa[NT], sb[NT], a[kFly][NT], b[kFly][NT];
+    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    uint32_t scale[TILES];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        sa[t] = *reinterpret_cast<const u4 *>(A.scales[t] + st * 16);
-        if (!One) sb[t] = *reinterpret_cast<const u4 *>(B.scales[t] + st * 16);
-    }
-    int from = 0, to = kSuper;
-    if (Edge) {
-        const int64_t e = stretch * kSuper;
-        from = lo <= e ? 0 : (lo - e < kSuper ? (int)(lo - e) : kSuper);
-        to = hi - e >= kSuper ? kSuper : (hi > e ? (int)(hi - e) : 0);
-    }
+    for (int t = 0; t < TILES; ++t) scale[t] = w.scale[t][4 * r + q];
+    const int u0 = from / n, units = (to - 1) / n - u0 + 1;      // (Uniform: that hold any)
 #pragma unroll
-    for (int j0 = 0; j0 < kUnits; j0 += kFly) {
+    for (int j = 0; j < 4; ++j) {
+        if (Masked && Uniform && units < 4 && ((j - u0) & 3) >= units) continue;
+        u4 code[TILES];
+        uint32_t byte[TILES];
 #pragma unroll
-        for (int j = 0; j < kFly; ++j) {
-            int64_t u = st * (4 * kUnits) + 4 * (j0 + j) + q;
-            if (Edge) u = u < last ? u : last;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                a[j][t] = *reinterpret_cast<const u4 *>(A.codes[t] + u * 16);
-                if (!One) b[j][t] = *reinterpret_cast<const u4 *>(B.codes[t] + u * 16);
-            }
+        for (int t = 0; t < TILES; ++t) {
+            code[t] = w.code[t][q][4 * r + (j ^ (r >> 2))];
+            byte[t] = (F == ADPSGD_MX_E2M1 ? scale[t] >> (8 * j) : scale[t] >> (8 * (j >> 1))) & 0xff;
         }
+        if (Masked) {
+            const int first = (4 * q + j) * n;
+            const bool none = first >= to || first + n <= from;
 #pragma unroll
-        for (int j = 0; j < kFly; ++j) {
-            uint32_t ba[NT], bb[NT];
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t m = none ? 0u : element_mask<kBits>(from - first, to - first, i);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                ba[t] = unit_scale<F>(sa[t], j0 + j);
-                if (!One) bb[t] = unit_scale<F>(sb[t], j0 + j);
+                for (int t = 0; t < TILES; ++t) code[t][i] &= m;
             }
-            if (Edge) {
-                const int first = (4 * (j0 + j) + q) * n;
-                const bool none = first >= to || first + n <= from;
+            // (none of this tensor's elements: neither is a NaN scale its own)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t m = none ? 0u : element_mask<kBits>(from - first, to - first, w);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        a[j][t][w] &= m;
-                        if (!One) b[j][t][w] &= m;
-                    }
-                }
-                // (none of this tensor's elements: neither is a NaN scale its own)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    ba[t] = none ? 127u : ba[t];
-                    if (!One) bb[t] = none ? 127u : bb[t];
-                }
-            }
-            multiply<F, NT, One>(a[j], ba, One ? a[j] : b[j], One ? ba : bb, acc);
+            for (int t = 0; t < TILES; ++t) byte[t] = none ? 127u : byte[t];
         }
-        if (kFly < kUnits) __builtin_amdgcn_sched_barrier(0);
+        multiply<F, NT, One>(code, byte, code + (One ? 0 : NT), byte + (One ? 0 : NT), acc);
+        // one step's masked or converted operands at a time
+        if (Masked || F == ADPSGD_MX_E4M3) __builtin_amdgcn_sched_barrier(0);
     }
 }
 
 // Groups of 16 NT rows that a block of the grid's second axis multiplies.
 enum { kDiagonal = 0, kAbove = 1, kEvery = 2 };
 
+// A wave walks through its chunk, 256 bytes of each row at a time, with the
+// tensors that meet it: their boundaries mask the elements in registers, and
+// where a tensor ends (or the chunk does) the accumulators are left as its
+// partial sum, or as its result if all of it lies in the chunk.  Where a whole
+// block's elements are one tensor's (the rule for long tensors), its four waves
+// leave one partial sum.
+//
 // NT: tiles of 16 rows of an operand that a wave holds at once.  kDiagonal: a
 // group with itself (b is a), tiles below the diagonal left out; kAbove: the
 // pairs of groups I < J (b is a); kEvery: all pairs.
 template <int F, int NT, int Pairs>
 __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     constexpr bool kOne = Pairs == kDiagonal;
-    constexpr int kWaves = kThreads / 64;
-    __shared__ float lds[kWaves][NT * NT][256];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    constexpr bool kPacked = NT == 1;         // (a tile may hold several stretches)
+    constexpr int TILES = kOne ? NT : 2 * NT, kElems = Fetch<F, NT>::kElems;
+    __shared__ WaveLds<TILES> shared[kProductWaves];
+    __shared__ float parts[kPacked ? kProductWaves * 256 : 1];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    WaveLds<TILES> &mine = shared[wave];
     const int32_t groups = (p.K + 16 * NT - 1) / (16 * NT);
     int32_t I = blockIdx.y, J = blockIdx.y;
     if (Pairs == kEvery) {
@@ -670,89 +706,206 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
         }
         J += I + 1;
     }
-    Lanes<NT> A, B;
-    A.point(p.ac, p.as, p.code_ld, p.scale_ld, I * 16 * NT, p.R, p.K);
-    if (!kOne) B.point(p.bc, p.bs, p.b_code_ld, p.b_scale_ld, J * 16 * NT, p.R, p.K);
-    const int32_t stretches = NT == 1 ? p.stretches : 1;
-    const int32_t mine = NT == 1 ? (lane & 15) / p.R : 0;
-    const int64_t super = (int64_t)stretches * kSuper;
-    for (uint32_t c = blockIdx.x; c < p.chunks; c += gridDim.x) {
-        const int64_t c0 = (int64_t)c * p.chunk;
-        const int64_t c1 = c0 + p.chunk < p.P ? c0 + p.chunk : p.P;
-        for (int32_t tau = tensor_at(p.off, p.T, c0); tau < p.T && p.off[tau] < c1; ++tau) {
-            int64_t lo = p.off[tau], hi = p.off[tau + 1];
-            lo = lo > c0 ? lo : c0;
-            hi = hi < c1 ? hi : c1;
-            if (hi <= lo) continue;
-            v4 acc[NT][NT];
+    Fetch<F, NT> a, o;
+    a.point(p.ac, p.as, p.code_ld, p.scale_ld, I * 16 * NT, p.R, p.K);
+    if (!kOne) o.point(p.bc, p.bs, p.b_code_ld, p.b_scale_ld, J * 16 * NT, p.R, p.K);
+    const int32_t stretches = kPacked ? p.stretches : 1;
+    const int32_t fetched = kPacked ? (lane >> 2) / p.R : 0, held = kPacked ? (lane & 15) / p.R : 0;   // stretch of a lane's row
+    const int64_t super = (int64_t)stretches * kElems;
+
+    v4 acc[NT][NT];
+    auto clear = [&] {
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
-            for (int64_t sb = lo / super + wave; sb * super < hi; sb += kWaves) {
-                const int64_t stretch = sb * stretches + mine;
-                if (sb * super >= lo && (sb + 1) * super <= hi)
-                    product_super<F, NT, kOne, false>(A, B, stretch, lo, hi, p.P, acc);
-                else
-                    product_super<F, NT, kOne, true>(A, B, stretch, lo, hi, p.P, acc);
+            for (int j = 0; j < NT; ++j) acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
+    };
+    auto park = [&](float *at) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int j = kOne ? i : 0; j < NT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    at[(i * NT + j) * 256 + (4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[i][j][r];
+    };
+    // Entry (y, x) of a K x K matrix; mirrored where b is a and tile (x, y) is not computed.
+    auto put = [&](float *out, bool mirror, int32_t y, int32_t x, float v) {
+        if (y >= p.K || x >= p.K) return;
+        out[(int64_t)y * p.K + x] = v;
+        if (Pairs != kEvery && mirror && y / 16 != x / 16) out[(int64_t)x * p.K + y] = v;
+    };
+    // One wave's accumulators to out.  (The addresses are worked out here each
+    // time: kept across the loops they would take more registers than the rest.)
+    auto leave = [&](float *out, bool mirror) {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        if (kPacked && stretches > 1) {      // the stretches' parts of the tile, summed
+            float *at = parts + wave * 256;
+            park(at);
+            __builtin_amdgcn_wave_barrier();
+            for (int e = l; e < p.R * p.R; e += 64) {
+                const int32_t row = e / p.R, col = e % p.R;
+                double s = 0.0;
+                for (int g = 0; g < stretches; ++g) s += at[(g * p.R + row) * 16 + g * p.R + col];
+                put(out, mirror, row, col, (float)s);
             }
-            // the waves' tiles (and the stretches' parts of one), summed, into the pair's partial sum
+            __builtin_amdgcn_wave_barrier();
+            return;
+        }
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int j = kOne ? i : 0; j < NT; ++j)
+            for (int j = kOne ? i : 0; j < NT; ++j)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        lds[wave][i * NT + j][(4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[i][j][r];
-            __syncthreads();
-            float *out = p.partials + ((int64_t)c + tau) * p.K * p.K;
-            const int32_t row = (int32_t)threadIdx.x / 16, col = (int32_t)threadIdx.x % 16;
-            if (NT == 1) {
-                if (I * 16 + row < p.K && J * 16 + col < p.K && row < p.R && col < p.R) {
-                    double s = 0.0;
-                    for (int w = 0; w < kWaves; ++w)
-                        for (int g = 0; g < stretches; ++g) s += lds[w][0][(g * p.R + row) * 16 + g * p.R + col];
-                    out[row * p.K + col] = (float)s;
+                for (int r = 0; r < 4; ++r)
+                    put(out, mirror, (I * NT + i) * 16 + 4 * (l >> 4) + r, (J * NT + j) * 16 + (l & 15), acc[i][j][r]);
+    };
+    const int64_t n = (int64_t)p.K * p.K;
+    for (uint32_t b = blockIdx.x; b < p.blocks; b += gridDim.x) {
+        const int64_t c = (int64_t)b * kProductWaves + wave;           // this wave's chunk
+        const int64_t b0 = (int64_t)b * kProductWaves * p.chunk, b1 = b0 + kProductWaves * p.chunk;
+        const int64_t c0 = c * p.chunk, c1 = c0 + p.chunk < p.P ? c0 + p.chunk : p.P;
+        int64_t s0 = c0;
+        a.template load<false>(s0 / kElems + fetched, p.P);
+        if (!kOne) o.template load<false>(s0 / kElems + fetched, p.P);
+        int32_t tau = tensor_at(p.off, p.T, b0);
+        clear();
+        if (p.off[tau] <= b0 && p.off[tau + 1] >= b1 && b1 <= p.P) {
+            while (s0 < c1) {
+                a.stash(mine, 0);
+                if (!kOne) o.stash(mine, NT);
+                s0 += super;
+                if (s0 < c1) {      // (on their way while these are multiplied)
+                    a.template load<true>(s0 / kElems + fetched, p.P);
+                    if (!kOne) o.template load<true>(s0 / kElems + fetched, p.P);
                 }
-            } else {
+                multiply_super<F, NT, kOne, false, true>(mine, 0, kElems, acc);
+            }
+            float *at = kPacked ? parts : reinterpret_cast<float *>(shared);
+            constexpr int kStride = kPacked ? 256 : sizeof(WaveLds<TILES>) / sizeof(float);   // of waves
+            park(at + wave * kStride);
+            __syncthreads();
+            float *out = p.partials + ((int64_t)b * kProductWaves + tau) * n;
+            int thread = threadIdx.x;
+            asm volatile("" : "+v"(thread));
+            const int32_t row = thread / 16, col = thread % 16;
+            if (!kPacked || (row < p.R && col < p.R)) {
 #pragma unroll
                 for (int i = 0; i < NT; ++i)
 #pragma unroll
                     for (int j = kOne ? i : 0; j < NT; ++j) {
-                        const int32_t y = (I * NT + i) * 16 + row, x = (J * NT + j) * 16 + col;
                         double s = 0.0;
-                        for (int w = 0; w < kWaves; ++w) s += lds[w][i * NT + j][threadIdx.x];
-                        if (y < p.K && x < p.K) out[(int64_t)y * p.K + x] = (float)s;
+                        for (int w = 0; w < kProductWaves; ++w)
+                            for (int g = 0; g < stretches; ++g)
+                                s += at[w * kStride + (i * NT + j) * 256 + (g * p.R + row) * 16 + g * p.R + col];
+                        put(out, false, (I * NT + i) * 16 + row, (J * NT + j) * 16 + col, (float)s);
                     }
             }
             __syncthreads();
+            continue;
         }
+        if (c0 >= p.P) continue;
+        // 64 boundaries at a time, lane i that of tensor from + i; the last tensor that begins by c0
+        int32_t from = tau;
+        int64_t bound = p.off[from + lane < p.T ? from + lane : p.T];
+        for (;;) {
+            const int32_t hits = __popcll(__ballot(from + lane < p.T && bound <= c0));
+            tau = from + (hits > 0 ? hits - 1 : 0);
+            if (hits < 64) break;
+            from = tau;
+            bound = p.off[from + lane < p.T ? from + lane : p.T];
+        }
+        bool open = false;             // acc holds something of tensor tau
+        while (s0 < c1) {
+            const int64_t s1 = s0 + super < c1 ? s0 + super : c1;
+            a.stash(mine, 0);
+            if (!kOne) o.stash(mine, NT);
+            if (s1 < c1) {
+                a.template load<false>(s1 / kElems + fetched, p.P);
+                if (!kOne) o.template load<false>(s1 / kElems + fetched, p.P);
+            }
+            while (tau < p.T) {
+                if (tau - from == 63) {
+                    from = tau;
+                    bound = p.off[tau + lane < p.T ? tau + lane : p.T];
+                }
+                const int64_t begin = lane_value(bound, tau - from), end = lane_value(bound, tau - from + 1);
+                if (begin >= s1) break;
+                const int64_t lo = begin > s0 ? begin : s0, hi = end < s1 ? end : s1;
+                if (hi > lo) {
+                    open = true;
+                    if (lo == s0 && hi == s0 + super) {
+                        multiply_super<F, NT, kOne, false, true>(mine, 0, kElems, acc);
+                    } else {
+                        // what of this lane's row is the tensor's
+                        const int first = held * kElems, f = (int)(lo - s0) - first, t = (int)(hi - s0) - first;
+                        multiply_super<F, NT, kOne, true, !kPacked>(mine, f < 0 ? 0 : f, t > kElems ? kElems : t, acc);
+                    }
+                }
+                if (end > s1) break;
+                if (open) {
+                    if (begin >= c0) leave(p.out + tau * n, true);        // (all of it was here)
+                    else leave(p.partials + (c + tau) * n, false);
+                    clear();
+                    open = false;
+                }
+                ++tau;
+            }
+            s0 = s1;
+        }
+        if (open) leave(p.partials + (c + tau) * n, false);
     }
 }
 
-// The tensors' sums of their chunks' partial sums, in 64 bits, by lanes of
-// `outs` entries: blockDim / outs of them share a tensor's chunks.  Where b is a,
+// The tensors' sums of the partial sums that k_mx_product left, in 64 bits, by
+// lanes of `outs` entries: blockDim / outs of them share a tensor's.  Where b is a,
 // tiles below the diagonal are the transposed ones above it.
 __global__ void __launch_bounds__(1024) k_mx_product_sum(const int64_t *off, const float *partials, int64_t chunk,
                                                          int64_t P, int32_t K, int32_t T, int same, int32_t outs,
                                                          float *out) {
     __shared__ double lds[1024];
-    const int64_t n = (int64_t)K * K;
+    const int64_t n = (int64_t)K * K, block = chunk * kProductWaves;
     const int32_t share = blockDim.x / outs, part = threadIdx.x / outs;
     const int64_t i = (int64_t)blockIdx.y * outs + threadIdx.x % outs;
     const int32_t row = (int32_t)(i / K), col = (int32_t)(i % K);
     const float *from = partials + (same && row / 16 > col / 16 ? (int64_t)col * K + row : i);
     for (int32_t tau = blockIdx.x; tau < T; tau += gridDim.x) {
         const int64_t lo = off[tau] > 0 ? off[tau] : 0, hi = off[tau + 1] < P ? off[tau + 1] : P;
-        double s[4] = {};
+        if (hi > lo && lo / chunk == (hi - 1) / chunk) continue;      // (one chunk: out has it)
+        double s = 0.0;
         if (hi > lo && i < n) {
-            const int64_t last = (hi - 1) / chunk;
-            int64_t c = lo / chunk + part;
-            for (; c + 3 * (int64_t)share <= last; c += 4 * (int64_t)share)
-                for (int u = 0; u < 4; ++u) s[u] += from[(c + u * (int64_t)share + tau) * n];
-            for (; c <= last; c += share) s[0] += from[(c + tau) * n];
+            // chunks before the tensor's whole blocks, one of each of those, chunks behind them
+            const int64_t first = lo / chunk, end = (hi - 1) / chunk + 1;
+            const int64_t b0 = (lo + block - 1) / block, b1 = hi / block;
+            auto add = [&](int64_t c, int64_t count, int32_t step) {
+                const float *at = from + (c + tau) * n;
+                const int64_t ld = step * n;
+                int32_t m = part;
+                for (; m + (kBatch - 1) * share < count; m += kBatch * share) {
+                    float v[kBatch];
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) v[u] = at[(int64_t)(m + u * share) * ld];
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) s += (double)v[u];
+                }
+                for (; m < count; m += 4 * share) {      // (loads without branches; past the end m's again)
+                    float v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[u] = at[(int64_t)(m + u * share < count ? m + u * share : m) * ld];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) s += m + u * share < count ? (double)v[u] : 0.0;
+                }
+            };
+            if (b1 > b0) {
+                add(first, b0 * kProductWaves - first, 1);
+                add(b0 * kProductWaves, b1 - b0, kProductWaves);
+                add(b1 * kProductWaves, end - b1 * kProductWaves, 1);
+            } else {
+                add(first, end - first, 1);
+            }
         }
-        lds[threadIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
+        lds[threadIdx.x] = s;
         __syncthreads();
         if (part == 0 && i < n) {
             double t = 0.0;
@@ -888,12 +1041,22 @@ int64_t average_chunk_elements(int64_t P) { return kThreads * 4 * (long_rows(P) 
 // Workers of a tile where several stretches share it.
 int32_t tile_workers(int32_t K) { return K > 8 ? 16 : K > 4 ? 8 : K > 2 ? 4 : K; }
 
-// Elements of a product block: 2048 blocks of a whole tile for each wave, at
-// most 16384 elements (of which fp32 sums are taken) for one wave.
+// Elements of a product's wave: 8192 waves (K = 8, P = 138M: 102 us; 115 us with
+// 4096, and with 16384 the sum of the partial sums takes 4 us more), fewer where
+// K x K partial sums of so many would come to more than 8 MB, or would outweigh
+// what the wave reads; and at most 16384 elements of a row (of which fp32 sums are
+// taken).
 int64_t product_chunk(int32_t K, int64_t P) {
-    const int64_t step = 4 * kSuper * (16 / tile_workers(K));
-    const int64_t n = (P / 2048 + step - 1) / step * step;
-    return n < step ? step : n > 65536 ? 65536 : n;
+    const int64_t super = kSuper * (16 / tile_workers(K));
+    const int64_t waves = std::max<int64_t>(std::min<int64_t>(8192, (int64_t(1) << 21) / ((int64_t)K * K)), 1);
+    const int64_t supers = (P + super - 1) / super;
+    const int64_t least = (15 * (int64_t)K + super - 1) / super;
+    return super * std::min<int64_t>(32, std::max<int64_t>(least, (supers + waves - 1) / waves));
+}
+
+int64_t product_blocks(int32_t K, int64_t P) {
+    const int64_t block = product_chunk(K, P) * kProductWaves;
+    return (P + block - 1) / block;
 }
 
 }  // namespace
@@ -956,13 +1119,12 @@ extern "C" int adpsgd_mx_quantize(const adpsgd_mx_rows *out, const float *x, int
 namespace {
 
 template <int F>
-void launch_dequantize(DequantizeParams &p, int32_t K, hipStream_t st) {
-    p.K = K;
-    p.groups = (uint32_t)((K + kReadRows - 1) / kReadRows);
+void launch_dequantize(DequantizeParams &p, hipStream_t st) {
+    p.groups = (uint32_t)((p.K + kReadRows - 1) / kReadRows);
     const uint32_t chunks = (uint32_t)((p.P + kReadChunk - 1) / kReadChunk);
     p.spread = chunks >= 8 ? 8 : 1;
     p.blocks = (chunks + p.spread - 1) / p.spread * p.spread * p.groups;
-    if (past_cache(K, p.P)) k_mx_dequantize<F, true><<<grid_for(p.blocks), kThreads, 0, st>>>(p);
+    if (past_cache(p.K, p.P)) k_mx_dequantize<F, true><<<grid_for(p.blocks), kThreads, 0, st>>>(p);
     else k_mx_dequantize<F, false><<<grid_for(p.blocks), kThreads, 0, st>>>(p);
 }
 
@@ -993,13 +1155,14 @@ extern "C" int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *bas
     p.codes = static_cast<const uint8_t *>(rows->codes);
     p.scales = static_cast<const uint8_t *>(rows->scales);
     p.base = base;
+    p.K = rows->K;
     p.y = y;
     p.code_ld = rows->code_stride;
     p.scale_ld = rows->scale_stride;
     p.P = P;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (rows->format == ADPSGD_MX_E2M1) launch_dequantize<ADPSGD_MX_E2M1>(p, rows->K, st);
-    else launch_dequantize<ADPSGD_MX_E4M3>(p, rows->K, st);
+    if (rows->format == ADPSGD_MX_E2M1) launch_dequantize<ADPSGD_MX_E2M1>(p, st);
+    else launch_dequantize<ADPSGD_MX_E4M3>(p, st);
     return launched("dequantize launch");
 }
 
@@ -1057,8 +1220,7 @@ extern "C" int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
 
 extern "C" size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T) {
     if (K < 1 || K > kMaxProductK || P < 0 || (P + 3) / 4 > (int64_t(1) << 32) || T < 1 || T > kMaxT) return 0;
-    const int64_t chunk = product_chunk(K, P);
-    return sizeof(float) * (size_t)((P + chunk - 1) / chunk + T) * K * K;
+    return sizeof(float) * (size_t)(product_blocks(K, P) * kProductWaves + T) * K * K;
 }
 
 namespace {
@@ -1066,21 +1228,20 @@ namespace {
 template <int F, int NT>
 void launch_product(const ProductParams &p, bool same, hipStream_t st) {
     const int32_t groups = (p.K + 16 * NT - 1) / (16 * NT);
-    const uint32_t x = grid_for(p.chunks);
+    const uint32_t x = grid_for(p.blocks);
     if (!same) {
         k_mx_product<F, NT, kEvery><<<dim3(x, groups * groups), kThreads, 0, st>>>(p);
         return;
     }
     k_mx_product<F, NT, kDiagonal><<<dim3(x, groups), kThreads, 0, st>>>(p);
-    if constexpr (NT == 4)
+    if constexpr (NT == 2)
         if (groups > 1) k_mx_product<F, NT, kAbove><<<dim3(x, groups * (groups - 1) / 2), kThreads, 0, st>>>(p);
 }
 
 template <int F>
 void launch_product(const ProductParams &p, bool same, hipStream_t st) {
     if (p.K <= 16) launch_product<F, 1>(p, same, st);
-    else if (p.K <= 32) launch_product<F, 2>(p, same, st);
-    else launch_product<F, 4>(p, same, st);
+    else launch_product<F, 2>(p, same, st);
 }
 
 }  // namespace
@@ -1110,13 +1271,14 @@ extern "C" int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *
     p.bs = static_cast<const uint8_t *>(b->scales);
     p.off = tensor_offsets;
     p.partials = static_cast<float *>(workspace);
+    p.out = out;
     p.code_ld = a->code_stride;
     p.scale_ld = a->scale_stride;
     p.b_code_ld = b->code_stride;
     p.b_scale_ld = b->scale_stride;
     p.P = P;
     p.chunk = product_chunk(a->K, P);
-    p.chunks = (uint32_t)((P + p.chunk - 1) / p.chunk);
+    p.blocks = (uint32_t)product_blocks(a->K, P);
     p.K = a->K;
     p.T = T;
     p.R = tile_workers(a->K);
@@ -1127,11 +1289,13 @@ extern "C" int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *
         else launch_product<ADPSGD_MX_E4M3>(p, same, st);
         if (int rc = launched("product launch")) return rc;
     }
-    // a block for each tensor and 64 entries; many threads to an entry where a tensor may have many chunks
-    const int64_t n = (int64_t)a->K * a->K;
-    int32_t outs = 1;
-    while (outs < 64 && outs < n) outs *= 2;
-    const uint32_t threads = (int64_t)p.chunks > 8 * (int64_t)T ? 1024 : kThreads;
+    // a block for each tensor and `outs` entries; more threads to an entry the more partial sums a tensor has
+    const int64_t n = (int64_t)a->K * a->K, items = (int64_t)p.blocks * kProductWaves / T;
+    int32_t outs = 1, share = 1;
+    while (outs < 1024 && outs < n) outs *= 2;
+    while (share < 1024 / std::min(outs, 64) && share * 8 < items) share *= 2;
+    while (outs * share > 1024) outs /= 2;
+    const uint32_t threads = (uint32_t)(outs * share);
     k_mx_product_sum<<<dim3(grid_for((uint64_t)T), (uint32_t)((n + outs - 1) / outs)), threads, 0, st>>>(
         tensor_offsets, p.partials, p.chunk, P, a->K, T, same, outs, out);
     return launched("product sum launch");
