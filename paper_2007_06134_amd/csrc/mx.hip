@@ -278,28 +278,35 @@ struct DequantizeParams {
     int64_t y_ld, code_ld, scale_ld;
     int64_t P;
     int32_t K;
-    uint32_t groups, blocks, spread;
+    uint32_t groups, chunks;     // of R rows, of kReadChunk elements
+    bool together;
 };
 
-// A block takes a chunk of the elements of up to kReadRows rows: base is loaded
-// once for them (K = 8, P = 138M: 1003 us; 1240 us with a row at a time).
-constexpr int kReadRows = 4;
+// A block takes a chunk of the elements of up to R rows.  The fewer rows are
+// written at a time the faster, but each group of R loads base again.  Times in
+// us at K = 8, P = 138M without and with base, K = 16, P = 25.6M (8 bits) without
+// and with:
+//   R = 2, a group of rows after another                  862, 1159, 327, 413
+//   R = 4, a group of rows after another                  899, 1045, 356, 378
+//   R = 4, the groups of one chunk together on one XCD    911, 1001, 374, 389
+// So two rows without base, and four with it: together where base is too
+// large to be kept by the cache from one group to the next.
 constexpr int kReadChunk = kThreads * 4;
-template <int F, bool NT, bool Full>
+template <int F, int R, bool NT, bool Full>
 __device__ __forceinline__ void dequantize_chunk(const DequantizeParams &p, int32_t k0, int64_t e) {
     using Code = typename Fmt<F>::Code;
     const int64_t at = Full || e < p.P ? e : (p.P - 1) / 4 * 4;
-    uint32_t c[kReadRows], s[kReadRows];
+    uint32_t c[R], s[R];
     f4 b = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kReadRows; ++i) {
+    for (int i = 0; i < R; ++i) {
         if (k0 + i >= p.K) break;
         c[i] = *reinterpret_cast<const Code *>(p.codes + (k0 + i) * p.code_ld + (at >> 2) * sizeof(Code));
         s[i] = p.scales[(k0 + i) * p.scale_ld + (at >> 5)];
     }
     if (p.base) b = load4<false, Full>(p.base, e, p.P);
 #pragma unroll
-    for (int i = 0; i < kReadRows; ++i) {
+    for (int i = 0; i < R; ++i) {
         if (k0 + i >= p.K) break;
         f4 v = Fmt<F>::decode(c[i], scale_of(s[i]));
         if (p.base) v = b + v;
@@ -307,16 +314,18 @@ __device__ __forceinline__ void dequantize_chunk(const DequantizeParams &p, int3
     }
 }
 
-template <int F, bool NT>
+template <int F, int R, bool NT>
 __global__ void __launch_bounds__(kThreads) k_mx_dequantize(DequantizeParams p) {
-    for (uint32_t b = blockIdx.x; b < p.blocks; b += gridDim.x) {
-        // the groups of rows of one chunk follow one another on one XCD
-        const uint32_t s = b / p.spread;
-        const int32_t k0 = (int32_t)(s % p.groups) * kReadRows;
-        const int64_t c0 = (int64_t)(s / p.groups * p.spread + b % p.spread) * kReadChunk;
+    for (uint32_t b = blockIdx.x; b < p.groups * p.chunks; b += gridDim.x) {
+        uint32_t group = b / p.chunks, chunk = b % p.chunks;
+        if (p.together) {                     // (chunks is a multiple of 8)
+            group = b / 8 % p.groups;
+            chunk = b / 8 / p.groups * 8 + b % 8;
+        }
+        const int64_t c0 = (int64_t)chunk * kReadChunk;
         if (c0 >= p.P) continue;
-        if (c0 + kReadChunk <= p.P) dequantize_chunk<F, NT, true>(p, k0, c0 + threadIdx.x * 4);
-        else dequantize_chunk<F, NT, false>(p, k0, c0 + threadIdx.x * 4);
+        if (c0 + kReadChunk <= p.P) dequantize_chunk<F, R, NT, true>(p, group * R, c0 + threadIdx.x * 4);
+        else dequantize_chunk<F, R, NT, false>(p, group * R, c0 + threadIdx.x * 4);
     }
 }
 
@@ -1029,8 +1038,11 @@ int launched(const char *what) {
 
 uint32_t grid_for(uint64_t blocks) { return (uint32_t)(blocks < kMaxGrid ? blocks : kMaxGrid); }
 
-// fp32 rows beyond the 256 MB last-level cache go past it.
-bool past_cache(int64_t K, int64_t P) { return (double)K * (double)P * 4.0 > 256e6; }
+// Rows of fp32 that would take most of the 256 MB last-level cache go past it
+// (quantize at K = 8, P = 4M with residuals in and out, 384 MB: 66 us, 75 us
+// through it); smaller ones may well be in it (average at K = 32, P = 1.2M,
+// 154 MB, of a model just worked on: 41 us, 50 us past it).
+bool past_cache(int64_t K, int64_t P, int arrays) { return (double)K * (double)P * 4.0 * arrays > 192e6; }
 
 // Several groups a lane for long rows (half the blocks' fixed work), one where
 // that would leave compute units without a block.
@@ -1105,7 +1117,7 @@ extern "C" int adpsgd_mx_quantize(const adpsgd_mx_rows *out, const float *x, int
     p.g = row_grid(out->K, P, 1);
     const dim3 grid(grid_for(p.g.blocks)), block(64);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const bool nt = past_cache(out->K, P);
+    const bool nt = past_cache(out->K, P, 1 + (residual_in != nullptr) + (residual_out && residual_out != residual_in));
     if (out->format == ADPSGD_MX_E2M1) {
         if (nt) k_mx_quantize<ADPSGD_MX_E2M1, true><<<grid, block, 0, st>>>(p);
         else k_mx_quantize<ADPSGD_MX_E2M1, false><<<grid, block, 0, st>>>(p);
@@ -1118,19 +1130,27 @@ extern "C" int adpsgd_mx_quantize(const adpsgd_mx_rows *out, const float *x, int
 
 namespace {
 
+template <int F, int R>
+void launch_dequantize(DequantizeParams &p, bool nt, hipStream_t st) {
+    p.groups = (uint32_t)((p.K + R - 1) / R);
+    const uint32_t grid = grid_for((uint64_t)p.groups * p.chunks);
+    if (nt) k_mx_dequantize<F, R, true><<<grid, kThreads, 0, st>>>(p);
+    else k_mx_dequantize<F, R, false><<<grid, kThreads, 0, st>>>(p);
+}
+
 template <int F>
 void launch_dequantize(DequantizeParams &p, hipStream_t st) {
-    p.groups = (uint32_t)((p.K + kReadRows - 1) / kReadRows);
-    const uint32_t chunks = (uint32_t)((p.P + kReadChunk - 1) / kReadChunk);
-    p.spread = chunks >= 8 ? 8 : 1;
-    p.blocks = (chunks + p.spread - 1) / p.spread * p.spread * p.groups;
-    if (past_cache(p.K, p.P)) k_mx_dequantize<F, true><<<grid_for(p.blocks), kThreads, 0, st>>>(p);
-    else k_mx_dequantize<F, false><<<grid_for(p.blocks), kThreads, 0, st>>>(p);
+    p.chunks = (uint32_t)((p.P + kReadChunk - 1) / kReadChunk);
+    p.together = p.base && past_cache(1, p.P, 1);
+    if (p.together) p.chunks = (p.chunks + 7) / 8 * 8;
+    const bool nt = past_cache(p.K, p.P, 1);
+    if (p.base && p.K > 2) launch_dequantize<F, 4>(p, nt, st);
+    else launch_dequantize<F, 2>(p, nt, st);
 }
 
 template <int F>
 void launch_average(const AverageParams &p, hipStream_t st) {
-    const bool nt = past_cache(p.K, p.P), several = long_rows(p.P);
+    const bool nt = past_cache(p.K, p.P, 1), several = long_rows(p.P);
     const uint32_t grid = grid_for(p.chunks);
     if (several && nt) k_mx_average<F, kAverageGroups, true><<<grid, kThreads, 0, st>>>(p);
     else if (several) k_mx_average<F, kAverageGroups, false><<<grid, kThreads, 0, st>>>(p);
