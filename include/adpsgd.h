@@ -383,7 +383,7 @@ typedef struct {
     int64_t code_stride;
     int64_t scale_stride;
     int64_t P;           /* >= 0                                    */
-    int32_t K;           /* in [1, 65536], K * P below 2^41         */
+    int32_t K;           /* in [1, 65536], K * P below 2^39         */
     int32_t format;      /* ADPSGD_MX_*                             */
 } adpsgd_mx_rows;
 
@@ -431,8 +431,8 @@ ADPSGD_API int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
  * b_k,i of the rows of two sets of messages of the same format, K <= 256 and P
  * (b NULL or a itself: of one set with itself, a symmetric matrix; then
  * (tr C - 1'C1 / K) / K is adpsgd_mx_average's variance).  Sums of up to 16384
- * products are taken in fp32, the rest in 64 bits.  An E4M3 element below
- * 2^-126 counts as zero.  tensor_offsets and workspace
+ * products are taken in fp32, the rest in 64 bits.  E4M3 elements below
+ * 2^-126 are rounded to multiples of 2^-133.  tensor_offsets and workspace
  * (adpsgd_mx_product_workspace bytes) as above.  Both workspace functions
  * return 0 for invalid arguments. */
 ADPSGD_API size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T);

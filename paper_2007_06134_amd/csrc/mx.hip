@@ -17,6 +17,8 @@
 // a table: no plan has to be built before a call.
 #include <hip/hip_runtime.h>
 
+#include <rocprofiler-sdk-roctx/roctx.h>
+
 #include <algorithm>
 #include <cstdint>
 #include <initializer_list>
@@ -37,7 +39,7 @@ constexpr int32_t kMaxProductK = 256;
 // Blocks a launch has at most; the kernels stride over the rest.  A multiple of
 // 8, so that a block's chunks stay on its XCD.
 constexpr uint32_t kMaxGrid = 1u << 23;
-constexpr int64_t kMaxPieces = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxPieces = (int64_t(1) << 31) - 1;   // of K rows (with what padding adds, a 32-bit block number)
 
 // Rows need not be 16-byte aligned: the hardware takes a 16-byte access at any
 // multiple of four.
@@ -178,30 +180,32 @@ __device__ __forceinline__ void store4(float *p, int64_t e, int64_t P, f4 v) {
 // are a row's pieces; an XCD takes `run` of its pieces of one row, then the
 // same pieces of the next row, so that base comes from memory once and from
 // that XCD's L2 for the other rows.
+// (K = 8, P = 138M with residuals: 2.29 ms; 2.48 ms with blocks of 8 KB of a row,
+// 2.72 ms with 16 KB.)
 constexpr int kPiece = 256;
 struct RowGrid {
     uint32_t K;
-    uint32_t slots;        // of a row: groups of spread NU pieces
+    uint32_t slots;        // of a row: groups of `spread` pieces
     uint32_t blocks;       // virtual blocks of the launch
     uint32_t spread;       // 8: pieces dealt to XCDs; 1: too few pieces for that
     uint32_t run;
 };
-RowGrid row_grid(int32_t K, int64_t P, int nu) {
+RowGrid row_grid(int32_t K, int64_t P) {
     RowGrid g;
     const int64_t pieces = (P + kPiece - 1) / kPiece;
     g.K = (uint32_t)K;
     g.spread = pieces >= 8 ? 8 : 1;
-    g.slots = (uint32_t)((pieces + g.spread * nu - 1) / (g.spread * nu));
-    g.run = g.slots >= 128u / nu ? 32u / nu : 1;
+    g.slots = (uint32_t)((pieces + g.spread - 1) / g.spread);
+    g.run = g.slots >= 128 ? 32 : 1;
     g.blocks = (g.slots + g.run - 1) / g.run * g.run * g.spread * g.K;
     return g;
 }
-// Block b's row and first piece (its further ones lie spread apart).
-__device__ __forceinline__ bool row_piece(const RowGrid &g, int nu, uint32_t b, uint32_t *k, uint32_t *piece) {
+// Block b's row and piece.
+__device__ __forceinline__ bool row_piece(const RowGrid &g, uint32_t b, uint32_t *k, uint32_t *piece) {
     const uint32_t s = b / g.spread, run = s / g.run;
     *k = run % g.K;
     const uint32_t slot = run / g.K * g.run + s % g.run;
-    *piece = slot * nu * g.spread + b % g.spread;
+    *piece = slot * g.spread + b % g.spread;
     return slot < g.slots;
 }
 
@@ -263,7 +267,7 @@ template <int F, bool NT>
 __global__ void __launch_bounds__(64) k_mx_quantize(QuantizeParams p) {
     for (uint32_t b = blockIdx.x; b < p.g.blocks; b += gridDim.x) {
         uint32_t k, piece;
-        if (!row_piece(p.g, 1, b, &k, &piece)) continue;
+        if (!row_piece(p.g, b, &k, &piece)) continue;
         const int64_t e0 = (int64_t)piece * kPiece, e = e0 + threadIdx.x * 4;
         if (e0 + kPiece <= p.P) quantize_piece<F, NT, true>(p, k, e);
         else quantize_piece<F, NT, false>(p, k, e);
@@ -342,12 +346,15 @@ struct AverageParams {
     int64_t P;
     uint32_t chunks;
     int32_t K, T;
+    double inv_k;
 };
 
 // Sums in 64 bits: of numbers with at most four significant bits the sums over
-// the workers, s1 of d and s2 of d^2, are exact unless their scales are 2^40
-// apart, so K s2 - s1^2 = K sum_k (d_k - mean)^2 loses nothing where the
-// workers agree, and one pass over the rows is enough.
+// the workers, s1 of d and s2 of d^2, are exact unless their scales are some 2^20
+// apart (where the smaller hardly count), so K s2 - s1^2 = K sum_k (d_k - mean)^2
+// loses nothing where the workers agree, and one pass over the rows is enough.
+// What bounds it is the writing of K rows: at K = 8, P = 138M 1.09 ms, 5.6 TB/s.
+// The codes of eight rows are loaded before any is used (a row at a time: 1.72 ms).
 constexpr int kRowsAtOnce = 8;     // rows whose codes are in flight together
 constexpr int kAverageGroups = 2;  // float4 groups of a lane in a large problem
 
@@ -401,14 +408,13 @@ __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0
             }
         }
     }
-    const double inv = 1.0 / (double)p.K;
     *all = 0.0;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         const int64_t e = e0 + u * (kThreads * 4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            b[u][j] = (float)((double)b[u][j] + s1[u][j] * inv);
+            b[u][j] = (float)((double)b[u][j] + s1[u][j] * p.inv_k);
             double q = (double)p.K * s2[u][j] - s1[u][j] * s1[u][j];
             q = Full || e + j < c1 ? (q < 0.0 ? 0.0 : q) : 0.0;    // (a NaN stays)
             s2[u][j] = q;
@@ -435,9 +441,9 @@ __global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
             if (threadIdx.x == 0) p.partials[(int64_t)c + tau] = all;
             continue;
         }
-        for (; tau < p.T && p.off[tau] < c1; ++tau) {
+        while (tau < p.T) {
             const int64_t lo = p.off[tau], hi = p.off[tau + 1];
-            if (hi <= lo || hi <= c0) continue;
+            if (lo >= c1) break;
             double part = 0.0;
 #pragma unroll
             for (int u = 0; u < NU; ++u)
@@ -448,6 +454,11 @@ __global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
                 }
             part = block_sum(part, lds);
             if (threadIdx.x == 0) p.partials[(int64_t)c + tau] = part;
+            if (hi >= c1) break;
+            // the tensor that goes on at hi, past any number of empty ones
+            const int32_t next = p.off[tau + 2 <= p.T ? tau + 2 : p.T] > hi ? tau + 1 : tensor_at(p.off, p.T, hi);
+            if (next <= tau) break;          // (not ascending)
+            tau = next;
         }
     }
 }
@@ -489,13 +500,15 @@ __global__ void __launch_bounds__(1024) k_mx_variance(const int64_t *off, const 
 //         the codes and applies both scales; its sums are rounded as fp32.
 //   E4M3: the 8-bit instructions drop products 2^-13 below the largest of
 //         their sum, so the codes are converted to bf16, exactly and with
-//         their scales (an element below 2^-126 becomes zero), for the bf16 instruction.
+//         their scales (an element below 2^-126 is rounded to bf16's subnormal
+//         numbers), for the bf16 instruction.
 // A lane of these instructions holds one row (lane mod 16), but lanes that load
-// 16 bytes of a row each cost an access of the vector cache each, and that many
-// accesses, not memory, set the time (K = 8, P = 138M: 43 million accesses,
-// 117 us).  So four lanes load 64 consecutive bytes of a row, and the units change
-// lanes through the wave's own part of LDS (units of a row rotated by the row
-// over 4, so that neither side meets bank conflicts).
+// 16 bytes of a row each cost an access of the vector cache each.  So four lanes
+// load 64 consecutive bytes of a row, a quarter of the accesses (K = 8, P = 138M:
+// 11 million, not 43), and the units change lanes through the wave's own part of
+// LDS, units of a row rotated by the row over 4, so that neither side meets bank
+// conflicts (K = 32, P = 20M: 72 us, 81 us without).  What bounds it is reading the
+// rows: at K = 8, P = 138M 101 us, 6.2 TB/s.
 // Where K <= 8, the 16 rows of the tile are 16 / R stretches of R = 1, 2, 4 or 8
 // workers: products of different stretches come out too and are left out.
 constexpr int kSuper = 512;
@@ -841,6 +854,11 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
                 }
                 const int64_t begin = lane_value(bound, tau - from), end = lane_value(bound, tau - from + 1);
                 if (begin >= s1) break;
+                if (end <= begin) {          // past the empty ones among the 64
+                    const uint64_t more = __ballot(bound > begin) & ~((uint64_t(2) << (tau - from)) - 1);
+                    tau = more ? from + __ffsll((unsigned long long)more) - 2 : from + 63;
+                    continue;
+                }
                 const int64_t lo = begin > s0 ? begin : s0, hi = end < s1 ? end : s1;
                 if (hi > lo) {
                     open = true;
@@ -989,7 +1007,7 @@ int check_rows(const adpsgd_mx_rows *r, const char *name) {
         return fail(ADPSGD_EINVAL, n + ".format must be ADPSGD_MX_E2M1 or ADPSGD_MX_E4M3");
     if (r->K < 1 || r->K > kMaxK) return fail(ADPSGD_EINVAL, "K must be in [1, 65536]");
     if (r->P < 0 || (r->P + 3) / 4 > (int64_t(1) << 32)) return fail(ADPSGD_EINVAL, "P must be >= 0 with P/4 below 2^32");
-    if ((r->P + 1023) / 1024 * r->K > kMaxPieces) return fail(ADPSGD_EINVAL, "K * P must be below 2^41");
+    if ((r->P + kPiece - 1) / kPiece > kMaxPieces / r->K) return fail(ADPSGD_EINVAL, "K * P must be below 2^39");
     const Bytes need = row_bytes(r->format, r->P);
     if (r->code_stride < need.codes || r->code_stride % 16 != 0)
         return fail(ADPSGD_EINVAL, n + ".code_stride must be a multiple of 16 and hold a row (" +
@@ -1029,6 +1047,11 @@ int check_workspace(const void *ws, size_t have, size_t need) {
     if (have < need) return fail(ADPSGD_EINVAL, "workspace needs " + std::to_string(need) + " bytes");
     return ADPSGD_OK;
 }
+
+struct Range {
+    explicit Range(const char *name) { roctxRangePushA(name); }
+    ~Range() { roctxRangePop(); }
+};
 
 int launched(const char *what) {
     const hipError_t e = hipGetLastError();
@@ -1087,6 +1110,7 @@ extern "C" int64_t adpsgd_mx_scale_stride(int64_t P) {
 
 extern "C" int adpsgd_mx_quantize(const adpsgd_mx_rows *out, const float *x, int64_t x_stride, const float *base,
                                   const float *residual_in, float *residual_out, int64_t residual_stride, void *stream) {
+    Range range_("adpsgd_mx_quantize");
     if (int rc = check_rows(out, "out")) return rc;
     const int64_t P = out->P;
     QuantizeParams p{};
@@ -1114,7 +1138,7 @@ extern "C" int adpsgd_mx_quantize(const adpsgd_mx_rows *out, const float *x, int
     p.code_ld = out->code_stride;
     p.scale_ld = out->scale_stride;
     p.P = P;
-    p.g = row_grid(out->K, P, 1);
+    p.g = row_grid(out->K, P);
     const dim3 grid(grid_for(p.g.blocks)), block(64);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool nt = past_cache(out->K, P, 1 + (residual_in != nullptr) + (residual_out && residual_out != residual_in));
@@ -1162,6 +1186,7 @@ void launch_average(const AverageParams &p, hipStream_t st) {
 
 extern "C" int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *base, float *y, int64_t y_stride,
                                     void *stream) {
+    Range range_("adpsgd_mx_dequantize");
     if (int rc = check_rows(rows, "rows")) return rc;
     const int64_t P = rows->P;
     DequantizeParams p{};
@@ -1195,6 +1220,7 @@ extern "C" size_t adpsgd_mx_average_workspace(int32_t K, int64_t P, int32_t T) {
 extern "C" int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const int64_t *tensor_offsets,
                                  const float *base, float *base_out, float *x, int64_t x_stride, double *var,
                                  void *workspace, size_t workspace_bytes, void *stream) {
+    Range range_("adpsgd_mx_average");
     if (int rc = check_rows(rows, "rows")) return rc;
     const int64_t P = rows->P;
     AverageParams p{};
@@ -1225,6 +1251,7 @@ extern "C" int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
     p.P = P;
     const int64_t chunk = average_chunk_elements(P);
     p.chunks = (uint32_t)((P + chunk - 1) / chunk);
+    p.inv_k = 1.0 / rows->K;
     p.K = rows->K;
     p.T = T;
     const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -1269,6 +1296,7 @@ void launch_product(const ProductParams &p, bool same, hipStream_t st) {
 extern "C" int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *b, int32_t T,
                                  const int64_t *tensor_offsets, float *out, void *workspace, size_t workspace_bytes,
                                  void *stream) {
+    Range range_("adpsgd_mx_product");
     if (int rc = check_rows(a, "a")) return rc;
     const bool same = !b || b == a || (b->codes == a->codes && b->scales == a->scales);
     if (b) {

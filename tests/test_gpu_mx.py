@@ -217,13 +217,16 @@ def _cuts(rng, P, kind):
     if kind == "edges":
         marks = [v + d for v in (32, 256, 512, 1024, 2048, 4096, 8192, 16384) for d in (-1, 0, 1) if v + d < P]
         return np.array([0] + sorted(marks) + [P])
+    if kind == "gaps":     # runs of empty tensors, longer than a wave's 64, at edges and anywhere
+        at = [0, 1, 1024, 1024, 2048, P - 1, P] + rng.integers(0, P + 1, 9).tolist()
+        return np.array([0] + sorted(v for a in at for v in [a] * int(rng.integers(1, 300))) + [P])
     n = int(min(P, 400))
     return np.array([0] + sorted(rng.integers(0, P + 1, n).tolist()) + [P])
 
 
 AVERAGE = [(1, 1, "one"), (2, 31, "empty"), (3, 33, "ones"), (8, 1025, "edges"), (5, 4099, "edges"), (16, 20_000, "many"),
            (33, 2000, "ones"), (100, 777, "many"), (3, 70_000, "empty"), (2, 4_300_007, "many"), (3, 4_200_000, "one"),
-           (7, 4_250_001, "edges")]
+           (7, 4_250_001, "edges"), (4, 5000, "gaps"), (3, 4_200_000, "gaps")]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -298,7 +301,8 @@ def _product_tol(off, mag):
 
 PRODUCT = [(1, 1, "one"), (2, 31, "empty"), (3, 33, "ones"), (8, 1025, "edges"), (16, 4099, "edges"), (17, 20_000, "many"),
            (32, 9000, "many"), (33, 2000, "ones"), (64, 3000, "edges"), (65, 2500, "many"), (100, 777, "many"),
-           (256, 600, "empty"), (4, 70_000, "empty"), (8, 300_007, "one"), (2, 4_300_007, "many"), (5, 2_000_000, "one")]
+           (256, 600, "empty"), (4, 70_000, "empty"), (8, 300_007, "one"), (2, 4_300_007, "many"), (5, 2_000_000, "one"),
+           (4, 5000, "gaps"), (20, 40_000, "gaps"), (40, 5000, "gaps")]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -336,6 +340,31 @@ def test_product_of_four_bit_messages_of_one_scale_is_exact(A, K):
     off = np.array([0, 1, 40, 5000, 5003, P])
     got = A.mx_product(rows, torch.from_numpy(off).cuda()).cpu().numpy()
     assert np.array_equal(got.astype(np.float64), ref.product(v, v, off)[0])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_product_of_far_scales(A, fmt):
+    """Rows of very large and very small numbers: their inner products are those of their scales, as far
+    as fp32 reaches (8-bit elements below 2^-126 are rounded to bf16's multiples of 2^-133)."""
+    P = 600
+    rng = np.random.default_rng(8)
+    bytes_ = np.array([0, 1, 20, 127, 190, 230])          # 2^-127 ... 2^103
+    codes, _, _ = _message(rng, 6, P, fmt)
+    byte = np.repeat(bytes_[:, None], -(-P // 32), 1).astype(np.uint8)
+    v = ref.values(codes, byte, P, fmt)
+    if fmt == ref.E4M3:
+        v = np.where(np.abs(v) < 2.0 ** -126, np.round(v * 2.0 ** 133) * 2.0 ** -133, v)
+    off = np.array([0, 100, P])
+    want, mag = ref.product(v, v, off)
+    got = A.mx_product(_rows(A, codes, byte, P, fmt), torch.from_numpy(off).cuda()).cpu().numpy().astype(np.float64)
+    fits = (mag < 2.0 ** 127) & (mag > 2.0 ** -100)       # no sum passes fp32, no product of weight is subnormal
+    assert fits.sum() > 20
+    # (a product below 2^-126 may be dropped: P of them)
+    off_by = (np.abs(got - want) - _product_tol(off, mag) - P * 2.0 ** -126)
+    _say(f"  past the tolerance: {[(tuple(i), got[tuple(i)], want[tuple(i)]) for i in np.argwhere((off_by > 0) & fits)[:6]]}")
+    assert np.all((off_by <= 0)[fits])
+    # products past fp32 are infinities, and of both signs their sum is NaN
+    assert not np.any(np.isfinite(got[mag > 2.0 ** 140]))
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
