@@ -528,15 +528,15 @@ struct ProductParams {
     int32_t R, stretches;  // 16 and 1 where K > 8
 };
 
+// The lowest n bits, n in [0, 32].
+__device__ __forceinline__ uint32_t low_bits(int n) { return n > 0 ? 0xffffffffu >> (32 - n) : 0u; }
+
 // Bits of the elements [a, b) of 32 / bits elements from w * (32 / bits) on.
 template <int bits>
 __device__ __forceinline__ uint32_t element_mask(int a, int b, int w) {
-    constexpr int per = 32 / bits;
-    a -= w * per;
-    b -= w * per;
-    a = a < 0 ? 0 : (a > per ? per : a);
-    b = b < 0 ? 0 : (b > per ? per : b);
-    return (uint32_t)((1ull << (bits * b)) - 1) & ~(uint32_t)((1ull << (bits * a)) - 1);
+    a = a * bits - 32 * w;
+    b = b * bits - 32 * w;
+    return low_bits(b > 32 ? 32 : b) & ~low_bits(a > 32 ? 32 : a);
 }
 
 // A unit of E4M3 codes as two operands of the bf16 instruction.
@@ -1340,7 +1340,7 @@ extern "C" int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *
     // a block for each tensor and `outs` entries; more threads to an entry the more partial sums a tensor has
     const int64_t n = (int64_t)a->K * a->K, items = (int64_t)p.blocks * kProductWaves / T;
     int32_t outs = 1, share = 1;
-    while (outs < 1024 && outs < n) outs *= 2;
+    while (outs < 128 && outs < n) outs *= 2;
     while (share < 1024 / std::min(outs, 64) && share * 8 < items) share *= 2;
     while (outs * share > 1024) outs /= 2;
     const uint32_t threads = (uint32_t)(outs * share);
