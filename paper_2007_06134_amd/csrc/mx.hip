@@ -1272,23 +1272,32 @@ extern "C" size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T) {
 
 namespace {
 
-template <int F, int NT>
-void launch_product(const ProductParams &p, bool same, hipStream_t st) {
-    const int32_t groups = (p.K + 16 * NT - 1) / (16 * NT);
-    const uint32_t x = grid_for(p.blocks);
-    if (!same) {
-        k_mx_product<F, NT, kEvery><<<dim3(x, groups * groups), kThreads, 0, st>>>(p);
-        return;
-    }
-    k_mx_product<F, NT, kDiagonal><<<dim3(x, groups), kThreads, 0, st>>>(p);
-    if constexpr (NT == 2)
-        if (groups > 1) k_mx_product<F, NT, kAbove><<<dim3(x, groups * (groups - 1) / 2), kThreads, 0, st>>>(p);
-}
-
+// Groups of rows by K: the more a wave holds, the fewer times the rows are loaded,
+// but the fewer waves a CU holds.  us, E2M1, b is a: K = 64, P = 5M 112 as two groups
+// of 32, 78 as one of 64; K = 33, P = 20M 179, 103 as one of 64, 91 as one of 48; but
+// K = 100, P = 0.5M 53 as groups of 32, 62 of 48 and 60 of 64.  Two operands (twice
+// the registers): K = 33, P = 5M 76 as groups of 32, 52 as one of 48; K = 100, P = 5M
+// 393 as four of 32, 301 as three of 48; K = 64 130 as two of 32, 144 as two of 48.
 template <int F>
 void launch_product(const ProductParams &p, bool same, hipStream_t st) {
-    if (p.K <= 16) launch_product<F, 1>(p, same, st);
-    else launch_product<F, 2>(p, same, st);
+    const uint32_t x = grid_for(p.blocks);
+    const uint32_t by32 = (p.K + 31) / 32, by48 = (p.K + 47) / 48;
+    if (!same) {
+        if (p.K <= 16) k_mx_product<F, 1, kEvery><<<x, kThreads, 0, st>>>(p);
+        else if (by48 < by32) k_mx_product<F, 3, kEvery><<<dim3(x, by48 * by48), kThreads, 0, st>>>(p);
+        else k_mx_product<F, 2, kEvery><<<dim3(x, by32 * by32), kThreads, 0, st>>>(p);
+        return;
+    }
+    if (p.K <= 16) {
+        k_mx_product<F, 1, kDiagonal><<<x, kThreads, 0, st>>>(p);
+    } else if (p.K <= 32 || p.K > 64) {
+        k_mx_product<F, 2, kDiagonal><<<dim3(x, by32), kThreads, 0, st>>>(p);
+        if (by32 > 1) k_mx_product<F, 2, kAbove><<<dim3(x, by32 * (by32 - 1) / 2), kThreads, 0, st>>>(p);
+    } else if (p.K <= 48) {
+        k_mx_product<F, 3, kDiagonal><<<x, kThreads, 0, st>>>(p);
+    } else {
+        k_mx_product<F, 4, kDiagonal><<<x, kThreads, 0, st>>>(p);
+    }
 }
 
 }  // namespace

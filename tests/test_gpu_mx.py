@@ -300,7 +300,8 @@ def _product_tol(off, mag):
 
 
 PRODUCT = [(1, 1, "one"), (2, 31, "empty"), (3, 33, "ones"), (8, 1025, "edges"), (16, 4099, "edges"), (17, 20_000, "many"),
-           (32, 9000, "many"), (33, 2000, "ones"), (64, 3000, "edges"), (65, 2500, "many"), (100, 777, "many"),
+           (32, 9000, "many"), (33, 2000, "ones"), (48, 30_000, "many"), (49, 3000, "many"), (64, 3000, "edges"), (65, 2500, "many"),
+           (96, 20_000, "edges"), (130, 1500, "empty"), (100, 777, "many"),
            (256, 600, "empty"), (4, 70_000, "empty"), (8, 300_007, "one"), (2, 4_300_007, "many"), (5, 2_000_000, "one"),
            (4, 5000, "gaps"), (20, 40_000, "gaps"), (40, 5000, "gaps")]
 
@@ -328,7 +329,7 @@ def test_product(A, fmt, K, P, cuts):
     assert np.all(np.abs(got - want) <= _product_tol(off, mag))
 
 
-@pytest.mark.parametrize("K", [1, 3, 8, 16, 20, 40, 70])
+@pytest.mark.parametrize("K", [1, 3, 8, 16, 20, 40, 60, 70])
 def test_product_of_four_bit_messages_of_one_scale_is_exact(A, K):
     """E2M1 products are quarters of integers up to 144: sums of 16384 of them fit an fp32 mantissa."""
     P = 16_384
