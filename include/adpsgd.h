@@ -375,8 +375,9 @@ ADPSGD_API int adpsgd_average_noalloc(int32_t K, int64_t P, int64_t row_stride, 
 /* K rows of P elements in device memory.  Row k's codes are 16 (E2M1) or 32
  * (E4M3) bytes a block at codes + k * code_stride, its scale bytes one a block
  * at scales + k * scale_stride; a row has ceil(P / 32) blocks.  Strides are in
- * bytes and multiples of 16, and both pointers are 16-byte aligned.  In a last
- * block that passes P the further elements are written as zero and not used. */
+ * bytes, multiples of 16 and at most 2^44 (as those of x and the residuals, in
+ * elements), and both pointers are 16-byte aligned.  In a last block that passes P
+ * the further elements are written as zero and not used. */
 typedef struct {
     void *codes;
     void *scales;
@@ -395,9 +396,9 @@ ADPSGD_API int64_t adpsgd_mx_scale_stride(int64_t P);
 /* Round d = (x - base) + residual_in to the format, every sum rounded to fp32:
  * a block's scale is the least power of two (at least 2^-127) that brings its
  * largest magnitude to at most 6 (E2M1) or 448 (E4M3), and an element the
- * nearest of the format's numbers that fp32 holds, ties to even.  residual_out = d - what was sent
- * (the error that the next message makes up for).  A block that holds a NaN or
- * an infinity is sent as NaN and leaves no residual.
+ * nearest of the format's numbers that fp32 holds, ties to even.  residual_out =
+ * d - what was sent (the error that the next message makes up for).  A block that
+ * holds a NaN or an infinity is sent as NaN and leaves no residual.
  * x [K][P] and the residuals [K][P] have rows x_stride and residual_stride
  * elements apart (0: P); base is [P].  base, residual_in (counted as zero) and
  * residual_out may be NULL; residual_out may be residual_in, else it overlaps no input. */
@@ -414,8 +415,8 @@ ADPSGD_API int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *bas
  * rows (one rounding to fp32), also written to every row of x [K][P] (rows
  * x_stride apart, 0: P), and var[tau] (device, [T]) = (1/K) sum_k sum_{i in
  * tau} (mean_i - row_k,i)^2 in 64 bits, as adpsgd_average's of the replicas base
- * + row.  base, base_out and x may be NULL; base_out may be
- * base; else no two of them overlap.
+ * + row.  base, base_out and x may be NULL; base_out may be base; else no two of
+ * them overlap.
  * tensor_offsets[T+1] is in device memory, as for adpsgd_init (T in [1, 2^24]);
  * its values are not read back: others than offsets[0] = 0 <= ... <=
  * offsets[T] = P give wrong sums, but touch nothing outside the arrays.

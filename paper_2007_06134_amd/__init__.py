@@ -119,6 +119,8 @@ class Adpsgd:
         torch = self.torch
         if self.hp.avg_momentum:
             raise ValueError("average_mx keeps the momentum local; the hyper-parameters ask for avg_momentum")
+        if products and self.K > 256:      # (before anything is sent)
+            raise ValueError("products are for at most 256 workers")
         with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
             if self.mx_base is None:
                 self.mx_base = torch.zeros((self.P,), device=self.device)

@@ -36,6 +36,7 @@ constexpr int kMxBlock = 32;           // elements that share a scale
 constexpr int32_t kMaxK = 65536;
 constexpr int32_t kMaxT = 1 << 24;
 constexpr int32_t kMaxProductK = 256;
+constexpr int64_t kMaxStride = int64_t(1) << 44;   // K rows of this many floats still have 63-bit addresses
 // Blocks a launch has at most; the kernels stride over the rest.  A multiple of
 // 8, so that a block's chunks stay on its XCD.
 constexpr uint32_t kMaxGrid = 1u << 23;
@@ -1009,11 +1010,11 @@ int check_rows(const adpsgd_mx_rows *r, const char *name) {
     if (r->P < 0 || (r->P + 3) / 4 > (int64_t(1) << 32)) return fail(ADPSGD_EINVAL, "P must be >= 0 with P/4 below 2^32");
     if ((r->P + kPiece - 1) / kPiece > kMaxPieces / r->K) return fail(ADPSGD_EINVAL, "K * P must be below 2^39");
     const Bytes need = row_bytes(r->format, r->P);
-    if (r->code_stride < need.codes || r->code_stride % 16 != 0)
-        return fail(ADPSGD_EINVAL, n + ".code_stride must be a multiple of 16 and hold a row (" +
+    if (r->code_stride < need.codes || r->code_stride % 16 != 0 || r->code_stride > kMaxStride)
+        return fail(ADPSGD_EINVAL, n + ".code_stride must be a multiple of 16, at most 2^44 and hold a row (" +
                                        std::to_string(need.codes) + " bytes)");
-    if (r->scale_stride < need.scales || r->scale_stride % 16 != 0)
-        return fail(ADPSGD_EINVAL, n + ".scale_stride must be a multiple of 16 and hold a row (" +
+    if (r->scale_stride < need.scales || r->scale_stride % 16 != 0 || r->scale_stride > kMaxStride)
+        return fail(ADPSGD_EINVAL, n + ".scale_stride must be a multiple of 16, at most 2^44 and hold a row (" +
                                        std::to_string(need.scales) + " bytes)");
     if (r->P > 0 && (!r->codes || !r->scales || !aligned16(r->codes) || !aligned16(r->scales)))
         return fail(ADPSGD_EINVAL, n + ".codes and .scales must be non-NULL and 16-byte aligned");
@@ -1022,8 +1023,8 @@ int check_rows(const adpsgd_mx_rows *r, const char *name) {
 
 // The row stride of a float array (0 means P).
 int check_ld(int64_t stride, int64_t P, const char *name, int64_t *ld) {
-    if (stride < 0 || (stride > 0 && stride < P))
-        return fail(ADPSGD_EINVAL, std::string(name) + " must be 0 or >= P");
+    if (stride < 0 || (stride > 0 && stride < P) || stride > kMaxStride)
+        return fail(ADPSGD_EINVAL, std::string(name) + " must be 0 or >= P, and at most 2^44");
     *ld = stride > 0 ? stride : P;
     return ADPSGD_OK;
 }

@@ -39,9 +39,10 @@ def _run(fn, dev: int, *args) -> None:
 
 class MxRows:
     """K rows of P elements: codes [K, >= ceil(P / 32) * 16 (E2M1) or * 32 (E4M3)] and scales
-    [K, >= ceil(P / 32)], uint8, rows at strides that are multiples of 16 bytes."""
+    [K, >= ceil(P / 32)], uint8, rows at strides that are multiples of 16 bytes.  The tensors keep their
+    memory for as long as the rows are used: what they hold may be written, they are not resized."""
 
-    __slots__ = ("codes", "scales", "P", "format", "K", "_dev", "_c", "_ref")
+    __slots__ = ("_codes", "_scales", "_P", "_format", "_K", "_dev", "_c", "_ref")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, P: int, format: int = MX_E2M1):
         per = _ROW_BYTES.get(format)
@@ -55,7 +56,7 @@ class MxRows:
         dev = codes.get_device()
         if K != K2 or scales.get_device() != dev:
             raise ValueError("codes and scales must have one row a worker on one device")
-        self.codes, self.scales, self.P, self.format, self.K, self._dev = codes, scales, P, format, K, dev
+        self._codes, self._scales, self._P, self._format, self._K, self._dev = codes, scales, P, format, K, dev
         self._c = adpsgd_mx_rows(codes.data_ptr(), scales.data_ptr(), code_ld, scale_ld, P, K, format)
         self._ref = C.byref(self._c)
 
@@ -69,9 +70,12 @@ class MxRows:
         return cls(torch.empty((K, lib.adpsgd_mx_code_stride(format, P)), dtype=_U8, device=device),
                    torch.empty((K, lib.adpsgd_mx_scale_stride(P)), dtype=_U8, device=device), P, format)
 
-    @property
-    def device(self) -> torch.device:
-        return self.codes.device
+    codes = property(lambda self: self._codes)
+    scales = property(lambda self: self._scales)
+    K = property(lambda self: self._K)
+    P = property(lambda self: self._P)
+    format = property(lambda self: self._format)
+    device = property(lambda self: self._codes.device)
 
 
 def _bytes(t: torch.Tensor, need: int, name: str) -> Tuple[int, int]:
@@ -140,7 +144,7 @@ def mx_quantize(x: torch.Tensor, base: Optional[torch.Tensor] = None, residual: 
         r_ld = ld
     if out is None:
         out = MxRows.empty(K, P, MX_E2M1 if format is None else format, x.device)
-    elif out.K != K or out.P != P or out._dev != dev or (format is not None and format != out.format):
+    elif out._K != K or out._P != P or out._dev != dev or (format is not None and format != out._format):
         raise ValueError(f"out must be rows of the format for [{K}, {P}] on device {dev}")
     _run(lib.adpsgd_mx_quantize, dev, out._ref, x.data_ptr(), x_ld, base_ptr, r_in, r_out, r_ld)
     return out
@@ -150,10 +154,10 @@ def mx_dequantize(rows: MxRows, base: Optional[torch.Tensor] = None, *,
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """What the rows say: base + their values, float32 [K, P]."""
     dev = rows._dev
-    base_ptr = _vector(base, rows.P, dev, "base")
+    base_ptr = _vector(base, rows._P, dev, "base")
     if out is None:
-        out = torch.empty((rows.K, rows.P), dtype=_F32, device=rows.device)
-    ld = _matrix(out, rows.K, rows.P, dev, "out")
+        out = torch.empty((rows._K, rows._P), dtype=_F32, device=rows._codes.device)
+    ld = _matrix(out, rows._K, rows._P, dev, "out")
     _run(lib.adpsgd_mx_dequantize, dev, rows._ref, base_ptr, out.data_ptr(), ld)
     return out
 
@@ -166,14 +170,14 @@ def mx_average(rows: MxRows, offsets: torch.Tensor, base: Optional[torch.Tensor]
     offsets: int64 [T + 1] on the device, the tensors' boundaries as for ``Adpsgd`` (0 first, P last;
     the values are not checked).  The new model is also written to every row of x [K, P] where that is
     given, and to base_out (which may be base; a new tensor by default)."""
-    dev, K, P = rows._dev, rows.K, rows.P
+    dev, K, P = rows._dev, rows._K, rows._P
     T = _offsets(offsets, dev)
     base_ptr = _vector(base, P, dev, "base")
     x_ptr, x_ld = None, 0
     if x is not None:
         x_ld, x_ptr = _matrix(x, K, P, dev, "x"), x.data_ptr()
     if base_out is None:
-        base_out = torch.empty((P,), dtype=_F32, device=rows.device)
+        base_out = torch.empty((P,), dtype=_F32, device=rows._codes.device)
     out_ptr = _vector(base_out, P, dev, "base_out")
     var = torch.empty((T,), dtype=_F64, device=offsets.device)
     need = lib.adpsgd_mx_average_workspace(K, P, T)
@@ -186,12 +190,12 @@ def mx_average(rows: MxRows, offsets: torch.Tensor, base: Optional[torch.Tensor]
 def mx_product(a: MxRows, offsets: torch.Tensor, b: Optional[MxRows] = None) -> torch.Tensor:
     """Inner products of the rows of a with those of b (of a, where b is None) for every tensor:
     float32 [T, K, K].  K is at most 256; a and b have the same format, K and P."""
-    dev, K = a._dev, a.K
+    dev, K = a._dev, a._K
     T = _offsets(offsets, dev)
     if b is not None and b._dev != dev:
         raise ValueError("a and b must be on one device")
     out = torch.empty((T, K, K), dtype=_F32, device=offsets.device)
-    need = lib.adpsgd_mx_product_workspace(K, a.P, T)
+    need = lib.adpsgd_mx_product_workspace(K, a._P, T)
     work = torch.empty((need,), dtype=_U8, device=offsets.device)
     _run(lib.adpsgd_mx_product, dev, a._ref, None if b is None else b._ref, T, offsets.data_ptr(), out.data_ptr(),
          work.data_ptr(), need)

@@ -633,6 +633,24 @@ def test_engine_sync_refuses_averaged_momentum(A):
             eng.average_mx()
 
 
+def test_engine_sync_refuses_too_many_products_before_it_sends(A):
+    w = _workload(K=257)
+    with A.Adpsgd.from_workload(w) as eng:
+        eng.local_steps(3)
+        x, cnt = eng.x.clone(), eng.get_state().cnt
+        with pytest.raises(ValueError):
+            eng.average_mx(products=True)
+        assert torch.equal(eng.x, x) and eng.get_state().cnt == cnt and eng.mx_residual is None
+        eng.average_mx()
+
+
+def test_rows_keep_what_they_were_made_of(A):
+    rows = A.mx_quantize(torch.ones((2, 40), device="cuda"))
+    for name in ("codes", "scales", "P", "K", "format"):
+        with pytest.raises(AttributeError):
+            setattr(rows, name, getattr(rows, name))
+
+
 def test_tensor_refusals(A):
     """What the Python calls refuse before anything runs."""
     K, P = 3, 100

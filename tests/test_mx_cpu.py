@@ -49,6 +49,23 @@ def test_rows_are_checked_by_every_call(A, lib, bad):
         assert call() == A.EINVAL and A.adpsgd_last_error()
 
 
+@pytest.mark.parametrize("K", [1, 4])
+def test_strides_whose_addresses_would_not_fit_are_refused(A, lib, K):
+    far, huge = 1 << 60, (1 << 44) + 16
+    for ld in (far, huge, (1 << 63) - 1):
+        r = C.byref(_rows(A, K=K))
+        calls = [lambda: lib.adpsgd_mx_quantize(r, BASE, ld, None, None, None, 0, None),
+                 lambda: lib.adpsgd_mx_quantize(r, BASE, 0, None, BASE, None, ld, None),
+                 lambda: lib.adpsgd_mx_dequantize(r, None, BASE, ld, None),
+                 lambda: lib.adpsgd_mx_average(r, 1, BASE, None, None, BASE, ld, BASE, BASE, 1 << 20, None)]
+        for name in ("code_stride", "scale_stride"):
+            if ld % 16 == 0:
+                bad = C.byref(_rows(A, K=K, **{name: ld}))
+                calls.append(lambda bad=bad: lib.adpsgd_mx_product(bad, None, 1, BASE, BASE, BASE, 1 << 30, None))
+        for call in calls:
+            assert call() == A.EINVAL and "2^44" in A.adpsgd_last_error()
+
+
 def test_null_rows(A, lib):
     assert lib.adpsgd_mx_quantize(None, BASE, 0, None, None, None, 0, None) == A.EINVAL
     assert lib.adpsgd_mx_dequantize(None, None, BASE, 0, None) == A.EINVAL
