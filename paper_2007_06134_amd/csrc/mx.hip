@@ -131,13 +131,6 @@ __device__ __forceinline__ int32_t tensor_at(const int64_t *off, int32_t T, int6
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Lane i's value, in scalar registers (i the same in all lanes).
-__device__ __forceinline__ int64_t lane_value(int64_t v, int i) {
-    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, i);
-    const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)v >> 32), i);
-    return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
 // A sum over the block's threads, in the same order every time; valid in thread 0.
 __device__ __forceinline__ double block_sum(double v, double *lds) {
 #pragma unroll
@@ -512,8 +505,11 @@ __global__ void __launch_bounds__(1024) k_mx_variance(const int64_t *off, const 
 // rows: at K = 8, P = 138M 101 us, 6.2 TB/s.
 // Where K <= 8, the 16 rows of the tile are 16 / R stretches of R = 1, 2, 4 or 8
 // workers: products of different stretches come out too and are left out.
+// Masks come from a table in LDS (three instructions a register of codes; from shifts
+// a dozen: 400 tensors of 32 workers 23 us, 20 us from the table).
 constexpr int kSuper = 512;
 constexpr int kProductWaves = kThreads / 64;
+constexpr int32_t kFar = 1 << 30;      // (a chunk is far shorter)
 
 struct ProductParams {
     const uint8_t *ac, *as, *bc, *bs;
@@ -526,19 +522,31 @@ struct ProductParams {
     int64_t chunk;         // a wave's elements, a multiple of stretches kSuper
     uint32_t blocks;       // of kProductWaves chunks
     int32_t K, T;
-    int32_t R, stretches;  // 16 and 1 where K > 8
+    int32_t R, stretches;  // 16 and 1 where K > 8 (and where P is small)
+    int32_t log_r;         // R = 2^log_r
 };
 
 // The lowest n bits, n in [0, 32].
 __device__ __forceinline__ uint32_t low_bits(int n) { return n > 0 ? 0xffffffffu >> (32 - n) : 0u; }
 
-// Bits of the elements [a, b) of 32 / bits elements from w * (32 / bits) on.
-template <int bits>
-__device__ __forceinline__ uint32_t element_mask(int a, int b, int w) {
-    a = a * bits - 32 * w;
-    b = b * bits - 32 * w;
-    return low_bits(b > 32 ? 32 : b) & ~low_bits(a > 32 ? 32 : a);
-}
+// A unit's masks: entry t's lowest t elements are set, by a block's first threads.
+template <int F>
+struct Masks {
+    static constexpr int kBits = F == ADPSGD_MX_E2M1 ? 4 : 8, kUnit = 128 / kBits;     // elements
+    u4 low[kUnit + 1];
+    __device__ __forceinline__ void make() {
+        const int t = threadIdx.x;
+        if (t > kUnit) return;
+        u4 m;
+        for (int i = 0; i < 4; ++i) {
+            const int n = t * kBits - 32 * i;
+            m[i] = low_bits(n < 32 ? n : 32);
+        }
+        low[t] = m;
+    }
+    // of the first n elements
+    __device__ __forceinline__ u4 first(int n) const { return low[n < 0 ? 0 : n > kUnit ? kUnit : n]; }
+};
 
 // A unit of E4M3 codes as two operands of the bf16 instruction.
 __device__ __forceinline__ void bf16_of(const u4 &v, uint32_t byte, bf8v *out) {
@@ -654,20 +662,19 @@ struct Fetch {
 
 // acc += the products of the elements [from, to) of the rows' kElems (Masked) or of
 // all.  Lane (row r = lane mod 16, q = lane / 16) takes unit 4 q + j of its row in
-// step j.  Uniform: from and to are the same in all lanes.
-template <int F, int NT, bool One, bool Masked, bool Uniform>
-__device__ __forceinline__ void multiply_super(const WaveLds<One ? NT : 2 * NT> &w, int from, int to,
-                                               v4 (&acc)[NT][NT]) {
-    constexpr int TILES = One ? NT : 2 * NT;
-    constexpr int kBits = F == ADPSGD_MX_E2M1 ? 4 : 8, n = 128 / kBits;
+// step j; only `units` consecutive ones from unit0 on hold any (both the same in all
+// lanes; of several rows' units in line).
+template <int F, int NT, bool One, bool Masked>
+__device__ __forceinline__ void multiply_super(const WaveLds<One ? NT : 2 * NT> &w, const Masks<F> &masks, int from,
+                                               int to, int unit0, int units, v4 (&acc)[NT][NT]) {
+    constexpr int TILES = One ? NT : 2 * NT, n = Masks<F>::kUnit;
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
     uint32_t scale[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) scale[t] = w.scale[t][4 * r + q];
-    const int u0 = from / n, units = (to - 1) / n - u0 + 1;      // (Uniform: that hold any)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        if (Masked && Uniform && units < 4 && ((j - u0) & 3) >= units) continue;
+        if (Masked && ((j - unit0) & 3) >= units) continue;
         u4 code[TILES];
         uint32_t byte[TILES];
 #pragma unroll
@@ -678,12 +685,9 @@ __device__ __forceinline__ void multiply_super(const WaveLds<One ? NT : 2 * NT> 
         if (Masked) {
             const int first = (4 * q + j) * n;
             const bool none = first >= to || first + n <= from;
+            const u4 m = masks.first(to - first) & ~masks.first(from - first);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t m = none ? 0u : element_mask<kBits>(from - first, to - first, i);
-#pragma unroll
-                for (int t = 0; t < TILES; ++t) code[t][i] &= m;
-            }
+            for (int t = 0; t < TILES; ++t) code[t] &= m;
             // (none of this tensor's elements: neither is a NaN scale its own)
 #pragma unroll
             for (int t = 0; t < TILES; ++t) byte[t] = none ? 127u : byte[t];
@@ -714,6 +718,7 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     constexpr int TILES = kOne ? NT : 2 * NT, kElems = Fetch<F, NT>::kElems;
     __shared__ WaveLds<TILES> shared[kProductWaves];
     __shared__ float parts[kPacked ? kProductWaves * 256 : 1];
+    __shared__ Masks<F> masks;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     WaveLds<TILES> &mine = shared[wave];
     const int32_t groups = (p.K + 16 * NT - 1) / (16 * NT);
@@ -768,7 +773,7 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
             park(at);
             __builtin_amdgcn_wave_barrier();
             for (int e = l; e < p.R * p.R; e += 64) {
-                const int32_t row = e / p.R, col = e % p.R;
+                const int32_t row = e >> p.log_r, col = e & (p.R - 1);
                 double s = 0.0;
                 for (int g = 0; g < stretches; ++g) s += at[(g * p.R + row) * 16 + g * p.R + col];
                 put(out, mirror, row, col, (float)s);
@@ -776,15 +781,28 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
             __builtin_amdgcn_wave_barrier();
             return;
         }
+        // (32-bit indexes from a scalar base; most matrices fill their tiles)
+        const uint32_t K = (uint32_t)p.K, y0 = I * 16 * NT + 4 * (l >> 4), x0 = J * 16 * NT + (l & 15), at = y0 * K + x0;
+        const bool whole = (uint32_t)((I + 1) * 16 * NT) <= K && (uint32_t)((J + 1) * 16 * NT) <= K;
+        auto store = [&](auto inside) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int j = kOne ? i : 0; j < NT; ++j)
+                for (int j = kOne ? i : 0; j < NT; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    put(out, mirror, (I * NT + i) * 16 + 4 * (l >> 4) + r, (J * NT + j) * 16 + (l & 15), acc[i][j][r]);
+                    for (int r = 0; r < 4; ++r) {
+                        if (!decltype(inside)::value && (y0 + 16 * i + r >= K || x0 + 16 * j >= K)) continue;
+                        out[at + (16 * i + r) * K + 16 * j] = acc[i][j][r];
+                        if (Pairs != kEvery && mirror && (Pairs == kAbove || i != j))
+                            out[(x0 + 16 * j) * K + y0 + 16 * i + r] = acc[i][j][r];
+                    }
+        };
+        if (whole) store(std::true_type{});
+        else store(std::false_type{});
     };
     const int64_t n = (int64_t)p.K * p.K;
+    masks.make();
+    __syncthreads();
     for (uint32_t b = blockIdx.x; b < p.blocks; b += gridDim.x) {
         const int64_t c = (int64_t)b * kProductWaves + wave;           // this wave's chunk
         const int64_t b0 = (int64_t)b * kProductWaves * p.chunk, b1 = b0 + kProductWaves * p.chunk;
@@ -803,7 +821,7 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
                     a.template load<true>(s0 / kElems + fetched, p.P);
                     if (!kOne) o.template load<true>(s0 / kElems + fetched, p.P);
                 }
-                multiply_super<F, NT, kOne, false, true>(mine, 0, kElems, acc);
+                multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
             }
             float *at = kPacked ? parts : reinterpret_cast<float *>(shared);
             constexpr int kStride = kPacked ? 256 : sizeof(WaveLds<TILES>) / sizeof(float);   // of waves
@@ -829,58 +847,68 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
             continue;
         }
         if (c0 >= p.P) continue;
-        // 64 boundaries at a time, lane i that of tensor from + i; the last tensor that begins by c0
-        int32_t from = tau;
-        int64_t bound = p.off[from + lane < p.T ? from + lane : p.T];
-        for (;;) {
-            const int32_t hits = __popcll(__ballot(from + lane < p.T && bound <= c0));
+        // From here on elements are counted from c0, in 32 bits (scalar ones: an int64 compare takes
+        // vector instructions); -1 and kFar stand for all before and far behind the chunk.
+        // 64 boundaries at a time, lane i that of tensor from + i.
+        auto boundary = [&](int32_t i) {
+            int64_t v = (int64_t)((uint64_t)p.off[i + lane < p.T ? i + lane : p.T] - (uint64_t)c0);
+            // (waited for here, not where it is used: with it all stores so far would be)
+            asm volatile("" : "+v"(v));
+            return v < 0 ? -1 : v < kFar ? (int32_t)v : kFar;
+        };
+        int32_t from = tau, bound = boundary(from);
+        for (;;) {                     // the last tensor that begins by c0
+            const int32_t hits = __popcll(__ballot(from + lane < p.T && bound <= 0));
             tau = from + (hits > 0 ? hits - 1 : 0);
             if (hits < 64) break;
             from = tau;
-            bound = p.off[from + lane < p.T ? from + lane : p.T];
+            bound = boundary(from);
         }
+        const int32_t span = (int32_t)super, size = (int32_t)(c1 - c0);
         bool open = false;             // acc holds something of tensor tau
-        while (s0 < c1) {
-            const int64_t s1 = s0 + super < c1 ? s0 + super : c1;
+        for (int32_t at = 0; at < size;) {
+            const int32_t next = at + span < size ? at + span : size;
             a.stash(mine, 0);
             if (!kOne) o.stash(mine, NT);
-            if (s1 < c1) {
-                a.template load<false>(s1 / kElems + fetched, p.P);
-                if (!kOne) o.template load<false>(s1 / kElems + fetched, p.P);
+            if (next < size) {
+                a.template load<false>((c0 + next) / kElems + fetched, p.P);
+                if (!kOne) o.template load<false>((c0 + next) / kElems + fetched, p.P);
             }
             while (tau < p.T) {
                 if (tau - from == 63) {
                     from = tau;
-                    bound = p.off[tau + lane < p.T ? tau + lane : p.T];
+                    bound = boundary(from);
                 }
-                const int64_t begin = lane_value(bound, tau - from), end = lane_value(bound, tau - from + 1);
-                if (begin >= s1) break;
+                const int32_t begin = __builtin_amdgcn_readlane(bound, tau - from);
+                const int32_t end = __builtin_amdgcn_readlane(bound, tau - from + 1);
+                if (begin >= next) break;
                 if (end <= begin) {          // past the empty ones among the 64
                     const uint64_t more = __ballot(bound > begin) & ~((uint64_t(2) << (tau - from)) - 1);
                     tau = more ? from + __ffsll((unsigned long long)more) - 2 : from + 63;
                     continue;
                 }
-                const int64_t lo = begin > s0 ? begin : s0, hi = end < s1 ? end : s1;
+                const int32_t lo = begin > at ? begin : at, hi = end < next ? end : next;
                 if (hi > lo) {
                     open = true;
-                    if (lo == s0 && hi == s0 + super) {
-                        multiply_super<F, NT, kOne, false, true>(mine, 0, kElems, acc);
+                    if (hi - lo == span) {
+                        multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
                     } else {
                         // what of this lane's row is the tensor's
-                        const int first = held * kElems, f = (int)(lo - s0) - first, t = (int)(hi - s0) - first;
-                        multiply_super<F, NT, kOne, true, !kPacked>(mine, f < 0 ? 0 : f, t > kElems ? kElems : t, acc);
+                        const int first = at + held * kElems, f = lo - first, t = hi - first;
+                        const int unit0 = (lo - at) / Masks<F>::kUnit, units = (hi - at - 1) / Masks<F>::kUnit - unit0 + 1;
+                        multiply_super<F, NT, kOne, true>(mine, masks, f < 0 ? 0 : f, t > kElems ? kElems : t, unit0, units, acc);
                     }
                 }
-                if (end > s1) break;
+                if (end > next) break;
                 if (open) {
-                    if (begin >= c0) leave(p.out + tau * n, true);        // (all of it was here)
+                    if (begin >= 0) leave(p.out + tau * n, true);        // (all of it was here)
                     else leave(p.partials + (c + tau) * n, false);
                     clear();
                     open = false;
                 }
                 ++tau;
             }
-            s0 = s1;
+            at = next;
         }
         if (open) leave(p.partials + (c + tau) * n, false);
     }
@@ -1074,8 +1102,14 @@ bool long_rows(int64_t P) { return P >= int64_t(1) << 22; }
 
 int64_t average_chunk_elements(int64_t P) { return kThreads * 4 * (long_rows(P) ? kAverageGroups : 1); }
 
-// Workers of a tile where several stretches share it.
-int32_t tile_workers(int32_t K) { return K > 8 ? 16 : K > 4 ? 8 : K > 2 ? 4 : K; }
+// Rows of a tile that a stretch takes: as many as there are workers, or more (the last
+// one repeated) where that few elements for so many stretches would make fewer than
+// 512 waves: K = 2, P = 1.2M in 400 tensors 22.5 us in 293 waves, 15.7 in 1172.
+int32_t tile_workers(int32_t K, int64_t P) {
+    int32_t R = K > 8 ? 16 : K > 4 ? 8 : K > 2 ? 4 : K;
+    while (R < 16 && P < 512 * kSuper * (16 / R)) R *= 2;
+    return R;
+}
 
 // Elements of a product's wave: 8192 waves (K = 8, P = 138M: 102 us; 115 us with
 // 4096, and with 16384 the sum of the partial sums takes 4 us more), fewer where
@@ -1083,7 +1117,7 @@ int32_t tile_workers(int32_t K) { return K > 8 ? 16 : K > 4 ? 8 : K > 2 ? 4 : K;
 // what the wave reads; and at most 16384 elements of a row (of which fp32 sums are
 // taken).
 int64_t product_chunk(int32_t K, int64_t P) {
-    const int64_t super = kSuper * (16 / tile_workers(K));
+    const int64_t super = kSuper * (16 / tile_workers(K, P));
     const int64_t waves = std::max<int64_t>(std::min<int64_t>(8192, (int64_t(1) << 21) / ((int64_t)K * K)), 1);
     const int64_t supers = (P + super - 1) / super;
     const int64_t least = (15 * (int64_t)K + super - 1) / super;
@@ -1339,8 +1373,9 @@ extern "C" int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *
     p.blocks = (uint32_t)product_blocks(a->K, P);
     p.K = a->K;
     p.T = T;
-    p.R = tile_workers(a->K);
+    p.R = tile_workers(a->K, P);
     p.stretches = 16 / p.R;
+    while (1 << p.log_r < p.R) ++p.log_r;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (P > 0) {
         if (a->format == ADPSGD_MX_E2M1) launch_product<ADPSGD_MX_E2M1>(p, same, st);

@@ -303,7 +303,9 @@ PRODUCT = [(1, 1, "one"), (2, 31, "empty"), (3, 33, "ones"), (8, 1025, "edges"),
            (32, 9000, "many"), (33, 2000, "ones"), (48, 30_000, "many"), (49, 3000, "many"), (64, 3000, "edges"), (65, 2500, "many"),
            (96, 20_000, "edges"), (130, 1500, "empty"), (100, 777, "many"),
            (256, 600, "empty"), (4, 70_000, "empty"), (8, 300_007, "one"), (2, 4_300_007, "many"), (5, 2_000_000, "one"),
-           (4, 5000, "gaps"), (20, 40_000, "gaps"), (40, 5000, "gaps")]
+           (4, 5000, "gaps"), (20, 40_000, "gaps"), (40, 5000, "gaps"),
+           # stretches that share a tile
+           (1, 4_400_000, "edges"), (3, 1_100_000, "many"), (4, 1_050_000, "gaps"), (7, 700_003, "many"), (8, 600_000, "edges")]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
