@@ -179,9 +179,9 @@ def mx_average(rows: MxRows, offsets: torch.Tensor, base: Optional[torch.Tensor]
     if base_out is None:
         base_out = torch.empty((P,), dtype=_F32, device=rows._codes.device)
     out_ptr = _vector(base_out, P, dev, "base_out")
-    var = torch.empty((T,), dtype=_F64, device=offsets.device)
+    var = offsets.new_empty(T, dtype=_F64)
     need = lib.adpsgd_mx_average_workspace(K, P, T)
-    work = torch.empty((need,), dtype=_U8, device=offsets.device)
+    work = offsets.new_empty(need + 7 >> 3)
     _run(lib.adpsgd_mx_average, dev, rows._ref, T, offsets.data_ptr(), base_ptr, out_ptr, x_ptr, x_ld, var.data_ptr(),
          work.data_ptr(), need)
     return base_out, var
@@ -194,9 +194,9 @@ def mx_product(a: MxRows, offsets: torch.Tensor, b: Optional[MxRows] = None) -> 
     T = _offsets(offsets, dev)
     if b is not None and b._dev != dev:
         raise ValueError("a and b must be on one device")
-    out = torch.empty((T, K, K), dtype=_F32, device=offsets.device)
+    out = offsets.new_empty((T, K, K), dtype=_F32)
     need = lib.adpsgd_mx_product_workspace(K, a._P, T)
-    work = torch.empty((need,), dtype=_U8, device=offsets.device)
+    work = offsets.new_empty(need + 7 >> 3)
     _run(lib.adpsgd_mx_product, dev, a._ref, None if b is None else b._ref, T, offsets.data_ptr(), out.data_ptr(),
          work.data_ptr(), need)
     return out
