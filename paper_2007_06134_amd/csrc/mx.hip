@@ -1111,14 +1111,14 @@ int32_t tile_workers(int32_t K, int64_t P) {
     return R;
 }
 
-// Elements of a product's wave: 8192 waves (K = 8, P = 138M: 102 us; 115 us with
-// 4096, and with 16384 the sum of the partial sums takes 4 us more), fewer where
-// K x K partial sums of so many would come to more than 8 MB, or would outweigh
-// what the wave reads; and at most 16384 elements of a row (of which fp32 sums are
-// taken).
+// Elements of a product's wave: 5120 waves, what the card holds at once of the kernels
+// for up to 16 workers (K = 8, P = 138M: 106 us; 108 with 8192, 115 with 4096; K = 16,
+// P = 25.6M, 8 bits: 86, 91 and 89), fewer where K x K partial sums of so many would
+// come to more than 8 MB, or would outweigh what the wave reads; and at most 16384
+// elements of a row (of which fp32 sums are taken).
 int64_t product_chunk(int32_t K, int64_t P) {
     const int64_t super = kSuper * (16 / tile_workers(K, P));
-    const int64_t waves = std::max<int64_t>(std::min<int64_t>(8192, (int64_t(1) << 21) / ((int64_t)K * K)), 1);
+    const int64_t waves = std::max<int64_t>(std::min<int64_t>(5120, (int64_t(1) << 21) / ((int64_t)K * K)), 1);
     const int64_t supers = (P + super - 1) / super;
     const int64_t least = (15 * (int64_t)K + super - 1) / super;
     return super * std::min<int64_t>(32, std::max<int64_t>(least, (supers + waves - 1) / waves));
