@@ -114,12 +114,13 @@ __device__ __forceinline__ uint32_t max_of_8_lanes(uint32_t v) {
     return o > v ? o : v;
 }
 
-// The last tensor that begins at or before element e (empty ones before it are
-// passed over), by all lanes of a wave: 64 offsets at a time.
-__device__ __forceinline__ int32_t tensor_at(const int64_t *off, int32_t T, int64_t e) {
+// Where tensors near element e begin: lane i gets tensor *from + i's first element (past
+// the last tensor P), the last one to begin by e being among the first 63.  By all
+// lanes of a wave, 64 offsets at a time.
+__device__ __forceinline__ int64_t offsets_near(const int64_t *off, int32_t T, int64_t e, int32_t *from) {
     int32_t lo = 0, n = T;
     const int lane = threadIdx.x & 63;
-    while (n > 1) {
+    while (n > 63) {
         const int32_t step = (n + 63) / 64;
         const int64_t i = (int64_t)lane * step;
         const uint64_t before = __ballot(i < n && off[lo + (i < n ? i : 0)] <= e);
@@ -128,13 +129,48 @@ __device__ __forceinline__ int32_t tensor_at(const int64_t *off, int32_t T, int6
         lo += at;
         n = n - at < step ? n - at : step;
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    *from = __builtin_amdgcn_readfirstlane(lo);
+    return off[*from + lane < T ? *from + lane : T];
+}
+
+// Element boundaries counted from c0 in 32 bits; -1 and kFar stand for all before it
+// and all far behind a chunk.
+constexpr int32_t kFar = 1 << 30;
+__device__ __forceinline__ int32_t boundary_from(int64_t off, int64_t c0) {
+    int64_t v = (int64_t)((uint64_t)off - (uint64_t)c0);
+    // (a loaded offset is waited for here: where it is used all stores so far would be, too)
+    asm volatile("" : "+v"(v));
+    return v < 0 ? -1 : v < kFar ? (int32_t)v : kFar;
+}
+
+// The last of the tensors from ... from + 62 that begins at or before the element that
+// lane i's bound of tensor from + i is counted from (else the first).
+__device__ __forceinline__ int32_t begun(int32_t bound, int32_t from, int32_t T) {
+    const int lane = threadIdx.x & 63;
+    const int32_t hits = __popcll(__ballot(lane < 63 && from + lane < T && bound <= 0));
+    return hits > 0 ? hits - 1 : 0;
+}
+
+// A sum over the wave's lanes, in the same order every time.
+__device__ __forceinline__ double wave_sum(double v) {
+    auto add = [&](auto ctrl) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, v);
+        constexpr int c = decltype(ctrl)::value;
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, c, 0xf, 0xf, true);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), c, 0xf, 0xf, true);
+        v += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    };
+    add(std::integral_constant<int, 0xB1>{});    // quad_perm 1,0,3,2
+    add(std::integral_constant<int, 0x4E>{});    // quad_perm 2,3,0,1
+    add(std::integral_constant<int, 0x141>{});   // mirrored halves of 16 lanes
+    add(std::integral_constant<int, 0x140>{});   // mirrored 16 lanes
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
 }
 
 // A sum over the block's threads, in the same order every time; valid in thread 0.
 __device__ __forceinline__ double block_sum(double v, double *lds) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    v = wave_sum(v);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     double t = 0.0;
@@ -354,7 +390,7 @@ constexpr int kAverageGroups = 2;  // float4 groups of a lane in a large problem
 
 template <int F, int NU, bool NT, bool Full>
 __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0, int64_t c1, double s2[NU][4],
-                                              int32_t *tau, double *all) {
+                                              int32_t *from, int32_t *bound) {
     using Code = typename Fmt<F>::Code;
     const int64_t e0 = c0 + threadIdx.x * 4;
     double s1[NU][4] = {};
@@ -367,6 +403,7 @@ __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0
         for (int j = 0; j < 4; ++j) s2[u][j] = 0.0;
     }
     f4 b[NU];
+    int64_t edge = 0;
     for (int32_t k0 = 0; k0 < p.K; k0 += kRowsAtOnce) {
         uint32_t c[kRowsAtOnce][NU], s[kRowsAtOnce][NU];
 #pragma unroll
@@ -385,7 +422,7 @@ __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0
                 b[u] = f4{0.f, 0.f, 0.f, 0.f};
                 if (p.base) b[u] = load4<false, Full>(p.base, e0 + u * (kThreads * 4), p.P);
             }
-            *tau = tensor_at(p.off, p.T, c0);
+            edge = offsets_near(p.off, p.T, c0, from);
         }
 #pragma unroll
         for (int i = 0; i < kRowsAtOnce; ++i) {
@@ -402,7 +439,7 @@ __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0
             }
         }
     }
-    *all = 0.0;
+    *bound = boundary_from(edge, c0);
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         const int64_t e = e0 + u * (kThreads * 4);
@@ -412,7 +449,6 @@ __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0
             double q = (double)p.K * s2[u][j] - s1[u][j] * s1[u][j];
             q = Full || e + j < c1 ? (q < 0.0 ? 0.0 : q) : 0.0;    // (a NaN stays)
             s2[u][j] = q;
-            *all += q;
         }
         if (p.base_out) store4<NT, Full>(p.base_out, e, p.P, b[u]);
         if (p.x)
@@ -420,40 +456,66 @@ __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0
     }
 }
 
+// Where several tensors meet a chunk, its squares go to LDS and each wave sums every
+// fourth tensor's (K = 8, P = 1.2M in 400 tensors: 17.0 us; 22.4 where the whole block
+// sums one tensor's after the other).
 template <int F, int NU, bool NT>
 __global__ void __launch_bounds__(kThreads) k_mx_average(AverageParams p) {
-    __shared__ double lds[kThreads / 64];
     constexpr int kChunk = kThreads * 4 * NU;
+    __shared__ double lds[kChunk];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (uint32_t c = blockIdx.x; c < p.chunks; c += gridDim.x) {
         const int64_t c0 = (int64_t)c * kChunk, c1 = c0 + kChunk < p.P ? c0 + kChunk : p.P;
-        double q[NU][4], all;
-        int32_t tau;
-        if (c0 + kChunk <= p.P) average_chunk<F, NU, NT, true>(p, c0, c1, q, &tau, &all);
-        else average_chunk<F, NU, NT, false>(p, c0, c1, q, &tau, &all);
-        if (p.off[tau + 1] >= c1) {
-            all = block_sum(all, lds);
-            if (threadIdx.x == 0) p.partials[(int64_t)c + tau] = all;
-            continue;
-        }
-        while (tau < p.T) {
-            const int64_t lo = p.off[tau], hi = p.off[tau + 1];
-            if (lo >= c1) break;
-            double part = 0.0;
+        const int32_t size = (int32_t)(c1 - c0);
+        double q[NU][4];
+        int32_t from, bound;       // lane i: where tensor from + i begins
+        if (c0 + kChunk <= p.P) average_chunk<F, NU, NT, true>(p, c0, c1, q, &from, &bound);
+        else average_chunk<F, NU, NT, false>(p, c0, c1, q, &from, &bound);
+        double *partials = p.partials + (int64_t)c;
+        const int32_t first = begun(bound, from, p.T);
+        if (__builtin_amdgcn_readlane(bound, first + 1) >= size) {
+            double all = 0.0;
 #pragma unroll
             for (int u = 0; u < NU; ++u)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int64_t e = c0 + threadIdx.x * 4 + u * (kThreads * 4) + j;
-                    if (e >= lo && e < hi) part += q[u][j];
-                }
-            part = block_sum(part, lds);
-            if (threadIdx.x == 0) p.partials[(int64_t)c + tau] = part;
-            if (hi >= c1) break;
-            // the tensor that goes on at hi, past any number of empty ones
-            const int32_t next = p.off[tau + 2 <= p.T ? tau + 2 : p.T] > hi ? tau + 1 : tensor_at(p.off, p.T, hi);
-            if (next <= tau) break;          // (not ascending)
-            tau = next;
+                for (int j = 0; j < 4; ++j) all += q[u][j];
+            all = block_sum(all, lds);
+            if (threadIdx.x == 0) partials[from + first] = all;
+            continue;
         }
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lds[u * (kThreads * 4) + threadIdx.x * 4 + j] = q[u][j];
+        __syncthreads();
+        for (int turn = wave;;) {
+            // the tensors among from ... from + 62 that hold some of the chunk
+            const int32_t end_of = __shfl_down(bound, 1, 64);
+            uint64_t some = __ballot(lane < 63 && from + lane < p.T && bound < end_of && end_of > 0 && bound < size);
+            for (; some; some &= some - 1, ++turn) {
+                if (turn % (kThreads / 64) != 0) continue;
+                const int i = __ffsll((unsigned long long)some) - 1;
+                const int32_t begin = __builtin_amdgcn_readlane(bound, i), end = __builtin_amdgcn_readlane(bound, i + 1);
+                const int32_t lo = begin > 0 ? begin : 0, hi = end < size ? end : size;
+                double part = 0.0;
+                for (int32_t e = lo + lane; e < hi; e += 64) part += lds[e];
+                part = wave_sum(part);
+                if (lane == 0) partials[from + i] = part;
+            }
+            const int32_t reached = __builtin_amdgcn_readlane(bound, 63);
+            if (reached >= size || from + 63 >= p.T) break;
+            // on at tensor from + 63, or past any number of empty ones
+            int32_t next;
+            const int64_t off = offsets_near(p.off, p.T, c0 + (reached > 0 ? reached : 0), &next);
+            if (next >= from + 63) {
+                from = next;
+                bound = boundary_from(off, c0);
+            } else {
+                from += 63;
+                bound = boundary_from(p.off[from + lane < p.T ? from + lane : p.T], c0);
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -509,7 +571,6 @@ __global__ void __launch_bounds__(1024) k_mx_variance(const int64_t *off, const 
 // a dozen: 400 tensors of 32 workers 23 us, 20 us from the table).
 constexpr int kSuper = 512;
 constexpr int kProductWaves = kThreads / 64;
-constexpr int32_t kFar = 1 << 30;      // (a chunk is far shorter)
 
 struct ProductParams {
     const uint8_t *ac, *as, *bc, *bs;
@@ -810,9 +871,12 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
         int64_t s0 = c0;
         a.template load<false>(s0 / kElems + fetched, p.P);
         if (!kOne) o.template load<false>(s0 / kElems + fetched, p.P);
-        int32_t tau = tensor_at(p.off, p.T, b0);
+        int32_t from;                  // lane i: where tensor from + i begins
+        int64_t edge = offsets_near(p.off, p.T, b0, &from);
         clear();
-        if (p.off[tau] <= b0 && p.off[tau + 1] >= b1 && b1 <= p.P) {
+        int32_t bound = boundary_from(edge, b0), tau = from + begun(bound, from, p.T);
+        if (__builtin_amdgcn_readlane(bound, tau - from) <= 0 && __builtin_amdgcn_readlane(bound, tau - from + 1) >= b1 - b0 &&
+            b1 <= p.P) {
             while (s0 < c1) {
                 a.stash(mine, 0);
                 if (!kOne) o.stash(mine, NT);
@@ -848,21 +912,15 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
         }
         if (c0 >= p.P) continue;
         // From here on elements are counted from c0, in 32 bits (scalar ones: an int64 compare takes
-        // vector instructions); -1 and kFar stand for all before and far behind the chunk.
-        // 64 boundaries at a time, lane i that of tensor from + i.
-        auto boundary = [&](int32_t i) {
-            int64_t v = (int64_t)((uint64_t)p.off[i + lane < p.T ? i + lane : p.T] - (uint64_t)c0);
-            // (waited for here, not where it is used: with it all stores so far would be)
-            asm volatile("" : "+v"(v));
-            return v < 0 ? -1 : v < kFar ? (int32_t)v : kFar;
-        };
-        int32_t from = tau, bound = boundary(from);
+        // vector instructions).  64 boundaries at a time, lane i that of tensor from + i.
+        auto boundary = [&](int32_t i) { return boundary_from(p.off[i + lane < p.T ? i + lane : p.T], c0); };
+        bound = boundary_from(edge, c0);
         for (;;) {                     // the last tensor that begins by c0
-            const int32_t hits = __popcll(__ballot(from + lane < p.T && bound <= 0));
-            tau = from + (hits > 0 ? hits - 1 : 0);
-            if (hits < 64) break;
+            tau = from + begun(bound, from, p.T);
+            if (tau < from + 62) break;
             from = tau;
             bound = boundary(from);
+            if (__builtin_amdgcn_readlane(bound, 1) > 0) break;
         }
         const int32_t span = (int32_t)super, size = (int32_t)(c1 - c0);
         bool open = false;             // acc holds something of tensor tau

@@ -214,6 +214,8 @@ def _cuts(rng, P, kind):
     if kind == "ones":
         n = min(P, 1500)
         return np.array(list(range(n)) + [P])
+    if kind == "singles":  # more tensors than two steps of 64 tell apart
+        return np.arange(P + 1)
     if kind == "edges":
         marks = [v + d for v in (32, 256, 512, 1024, 2048, 4096, 8192, 16384) for d in (-1, 0, 1) if v + d < P]
         return np.array([0] + sorted(marks) + [P])
@@ -226,7 +228,7 @@ def _cuts(rng, P, kind):
 
 AVERAGE = [(1, 1, "one"), (2, 31, "empty"), (3, 33, "ones"), (8, 1025, "edges"), (5, 4099, "edges"), (16, 20_000, "many"),
            (33, 2000, "ones"), (100, 777, "many"), (3, 70_000, "empty"), (2, 4_300_007, "many"), (3, 4_200_000, "one"),
-           (7, 4_250_001, "edges"), (4, 5000, "gaps"), (3, 4_200_000, "gaps")]
+           (7, 4_250_001, "edges"), (4, 5000, "gaps"), (3, 4_200_000, "gaps"), (2, 20_000, "singles")]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -305,7 +307,8 @@ PRODUCT = [(1, 1, "one"), (2, 31, "empty"), (3, 33, "ones"), (8, 1025, "edges"),
            (256, 600, "empty"), (4, 70_000, "empty"), (8, 300_007, "one"), (2, 4_300_007, "many"), (5, 2_000_000, "one"),
            (4, 5000, "gaps"), (20, 40_000, "gaps"), (40, 5000, "gaps"),
            # stretches that share a tile
-           (1, 4_400_000, "edges"), (3, 1_100_000, "many"), (4, 1_050_000, "gaps"), (7, 700_003, "many"), (8, 600_000, "edges")]
+           (1, 4_400_000, "edges"), (3, 1_100_000, "many"), (4, 1_050_000, "gaps"), (7, 700_003, "many"), (8, 600_000, "edges"),
+           (2, 20_000, "singles"), (17, 10_000, "singles")]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
