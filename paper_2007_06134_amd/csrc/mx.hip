@@ -383,15 +383,17 @@ struct AverageParams {
 // the workers, s1 of d and s2 of d^2, are exact unless their scales are some 2^20
 // apart (where the smaller hardly count), so K s2 - s1^2 = K sum_k (d_k - mean)^2
 // loses nothing where the workers agree, and one pass over the rows is enough.
-// What bounds it is the writing of K rows: at K = 8, P = 138M 1.09 ms, 5.6 TB/s.
-// The codes of eight rows are loaded before any is used (a row at a time: 1.72 ms).
-constexpr int kRowsAtOnce = 8;     // rows whose codes are in flight together
+// What bounds it is the writing of K rows: at K = 8, P = 138M 1.08 ms, 5.6 TB/s.
+// The codes of eight rows are loaded before any is used (a row at a time: 1.72 ms), of
+// sixteen where a lane has one group of each (K = 32, P = 1.2M, 8 bits: 47.8 us; 49.2
+// with eight, 49.2 with 32).
 constexpr int kAverageGroups = 2;  // float4 groups of a lane in a large problem
 
 template <int F, int NU, bool NT, bool Full>
 __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0, int64_t c1, double s2[NU][4],
                                               int32_t *from, int32_t *bound) {
     using Code = typename Fmt<F>::Code;
+    constexpr int kRowsAtOnce = NU == 1 ? 16 : 8;     // whose codes are in flight together
     const int64_t e0 = c0 + threadIdx.x * 4;
     double s1[NU][4] = {};
     int64_t at[NU];
