@@ -210,7 +210,7 @@ __device__ __forceinline__ void store4(float *p, int64_t e, int64_t P, f4 v) {
 // are a row's pieces; an XCD takes `run` of its pieces of one row, then the
 // same pieces of the next row, so that base comes from memory once and from
 // that XCD's L2 for the other rows.
-// (K = 8, P = 138M with residuals: 2.29 ms; 2.48 ms with blocks of 8 KB of a row,
+// (K = 8, P = 138M with residuals: 2.24-2.29 ms; 2.48 ms with blocks of 8 KB of a row,
 // 2.72 ms with 16 KB.)
 constexpr int kPiece = 256;
 struct RowGrid {
@@ -566,7 +566,7 @@ __global__ void __launch_bounds__(1024) k_mx_variance(const int64_t *off, const 
 // 11 million, not 43), and the units change lanes through the wave's own part of
 // LDS, units of a row rotated by the row over 4, so that neither side meets bank
 // conflicts (K = 32, P = 20M: 72 us, 81 us without).  What bounds it is reading the
-// rows: at K = 8, P = 138M 101 us, 6.2 TB/s.
+// rows: at K = 8, P = 138M 99-104 us, 5.6-5.9 TB/s.
 // Where K <= 8, the 16 rows of the tile are 16 / R stretches of R = 1, 2, 4 or 8
 // workers: products of different stretches come out too and are left out.
 // Masks come from a table in LDS (three instructions a register of codes; from shifts
