@@ -1171,17 +1171,22 @@ int32_t tile_workers(int32_t K, int64_t P) {
     return R;
 }
 
-// Elements of a product's wave: 5120 waves, what the card holds at once of the kernels
-// for up to 16 workers (K = 8, P = 138M: 106 us; 108 with 8192, 115 with 4096; K = 16,
-// P = 25.6M, 8 bits: 86, 91 and 89), fewer where K x K partial sums of so many would
-// come to more than 8 MB, or would outweigh what the wave reads; and at most 16384
-// elements of a row (of which fp32 sums are taken).
+// Elements of a product's wave: of as many waves as the compute units hold evenly, four to
+// a block and 256 blocks a step.  20 waves a unit of the kernels for up to 16 workers
+// (K = 8, P = 138M: 106 us; 108 with 32, 115 with 16; K = 16, P = 25.6M, 8 bits: 86, 91
+// and 89), 8 for up to 32 (K = 24, P = 5M: 29 us; 36 with 13, 31 with 12, 27 with 4, but
+// K = 32, P = 20M 78 with 8 and 92 with 4), 4 for up to 64 (K = 64, P = 5M: 55 us; 66
+// with 2; two sets of 40, P = 10M, 8 bits: 160, and 197 with 5), and a whole number of
+// fours where more are needed (two sets of 40, P = 20M: 161 us with 8, 203 with 5).
+// More workers fill the units with pairs of groups: fewer waves, so that the K x K
+// partial sums come to 8 MB at most.  No wave takes less than its partial sums outweigh,
+// nor more than 16384 elements of a row (of which fp32 sums are taken).
 int64_t product_chunk(int32_t K, int64_t P) {
-    const int64_t super = kSuper * (16 / tile_workers(K, P));
-    const int64_t waves = std::max<int64_t>(std::min<int64_t>(5120, (int64_t(1) << 21) / ((int64_t)K * K)), 1);
-    const int64_t supers = (P + super - 1) / super;
-    const int64_t least = (15 * (int64_t)K + super - 1) / super;
-    return super * std::min<int64_t>(32, std::max<int64_t>(least, (supers + waves - 1) / waves));
+    const int64_t super = kSuper * (16 / tile_workers(K, P)), most = 32;
+    const int64_t supers = (P + super - 1) / super, least = (15 * (int64_t)K + super - 1) / super;
+    int64_t waves = K <= 16 ? 5120 : K <= 32 ? 2048 : K <= 64 ? 1024 : (int64_t(1) << 21) / ((int64_t)K * K);
+    if (K <= 64 && supers > most * waves) waves = (supers + most * 1024 - 1) / (most * 1024) * 1024;
+    return super * std::min<int64_t>(most, std::max<int64_t>(least, (supers + waves - 1) / waves));
 }
 
 int64_t product_blocks(int32_t K, int64_t P) {
