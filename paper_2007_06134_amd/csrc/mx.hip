@@ -584,6 +584,7 @@ struct ProductParams {
     int64_t P;
     int64_t chunk;         // a wave's elements, a multiple of stretches kSuper
     uint32_t blocks;       // of kProductWaves chunks
+    uint32_t pairs;        // of groups of rows
     int32_t K, T;
     int32_t R, stretches;  // 16 and 1 where K > 8 (and where P is small)
     int32_t log_r;         // R = 2^log_r
@@ -761,8 +762,9 @@ __device__ __forceinline__ void multiply_super(const WaveLds<One ? NT : 2 * NT> 
     }
 }
 
-// Groups of 16 NT rows that a block of the grid's second axis multiplies.
-enum { kDiagonal = 0, kAbove = 1, kEvery = 2 };
+// Which groups of 16 NT rows are multiplied: one group with itself (b is a), the pairs
+// of groups I <= J (b is a), all pairs.
+enum { kOneGroup = 0, kUpper = 1, kEvery = 2 };
 
 // A wave walks through its chunk, 256 bytes of each row at a time, with the
 // tensors that meet it: their boundaries mask the elements in registers, and
@@ -771,12 +773,13 @@ enum { kDiagonal = 0, kAbove = 1, kEvery = 2 };
 // block's elements are one tensor's (the rule for long tensors), its four waves
 // leave one partial sum.
 //
-// NT: tiles of 16 rows of an operand that a wave holds at once.  kDiagonal: a
-// group with itself (b is a), tiles below the diagonal left out; kAbove: the
-// pairs of groups I < J (b is a); kEvery: all pairs.
+// NT: tiles of 16 rows of an operand that a wave holds at once (of one group, those
+// below the diagonal are left out).  The pairs of groups of the same elements follow each
+// other on one XCD, whose L2 gives the rows to all but the first (K = 256, P = 4M 767 ->
+// 430 us; two sets of 128, P = 5M 359 -> 230).
 template <int F, int NT, int Pairs>
 __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
-    constexpr bool kOne = Pairs == kDiagonal;
+    constexpr bool kOne = Pairs == kOneGroup;
     constexpr bool kPacked = NT == 1;         // (a tile may hold several stretches)
     constexpr int TILES = kOne ? NT : 2 * NT, kElems = Fetch<F, NT>::kElems;
     __shared__ WaveLds<TILES> shared[kProductWaves];
@@ -785,17 +788,15 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     WaveLds<TILES> &mine = shared[wave];
     const int32_t groups = (p.K + 16 * NT - 1) / (16 * NT);
-    int32_t I = blockIdx.y, J = blockIdx.y;
+    const uint32_t pair = blockIdx.x / 8 % p.pairs, b = blockIdx.x / 8 / p.pairs * 8 + blockIdx.x % 8;
+    if (b >= p.blocks) return;
+    int32_t I = 0, J = 0;
     if (Pairs == kEvery) {
-        I = blockIdx.y / groups;
-        J = blockIdx.y % groups;
-    } else if (Pairs == kAbove) {
-        I = 0;
-        while (J >= groups - 1 - I) {
-            J -= groups - 1 - I;
-            ++I;
-        }
-        J += I + 1;
+        I = pair / groups;
+        J = pair % groups;
+    } else if (Pairs == kUpper) {
+        for (J = pair; J >= groups - I; ++I) J -= groups - I;
+        J += I;
     }
     Fetch<F, NT> a, o;
     a.point(p.ac, p.as, p.code_ld, p.scale_ld, I * 16 * NT, p.R, p.K);
@@ -856,7 +857,7 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
                     for (int r = 0; r < 4; ++r) {
                         if (!decltype(inside)::value && (y0 + 16 * i + r >= K || x0 + 16 * j >= K)) continue;
                         out[at + (16 * i + r) * K + 16 * j] = acc[i][j][r];
-                        if (Pairs != kEvery && mirror && (Pairs == kAbove || i != j))
+                        if (Pairs != kEvery && mirror && (Pairs == kUpper ? I != J : i != j))
                             out[(x0 + 16 * j) * K + y0 + 16 * i + r] = acc[i][j][r];
                     }
         };
@@ -866,112 +867,109 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     const int64_t n = (int64_t)p.K * p.K;
     masks.make();
     __syncthreads();
-    for (uint32_t b = blockIdx.x; b < p.blocks; b += gridDim.x) {
-        const int64_t c = (int64_t)b * kProductWaves + wave;           // this wave's chunk
-        const int64_t b0 = (int64_t)b * kProductWaves * p.chunk, b1 = b0 + kProductWaves * p.chunk;
-        const int64_t c0 = c * p.chunk, c1 = c0 + p.chunk < p.P ? c0 + p.chunk : p.P;
-        int64_t s0 = c0;
-        a.template load<false>(s0 / kElems + fetched, p.P);
-        if (!kOne) o.template load<false>(s0 / kElems + fetched, p.P);
-        int32_t from;                  // lane i: where tensor from + i begins
-        int64_t edge = offsets_near(p.off, p.T, b0, &from);
-        clear();
-        int32_t bound = boundary_from(edge, b0), tau = from + begun(bound, from, p.T);
-        if (__builtin_amdgcn_readlane(bound, tau - from) <= 0 && __builtin_amdgcn_readlane(bound, tau - from + 1) >= b1 - b0 &&
-            b1 <= p.P) {
-            while (s0 < c1) {
-                a.stash(mine, 0);
-                if (!kOne) o.stash(mine, NT);
-                s0 += super;
-                if (s0 < c1) {      // (on their way while these are multiplied)
-                    a.template load<true>(s0 / kElems + fetched, p.P);
-                    if (!kOne) o.template load<true>(s0 / kElems + fetched, p.P);
-                }
-                multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
-            }
-            float *at = kPacked ? parts : reinterpret_cast<float *>(shared);
-            constexpr int kStride = kPacked ? 256 : sizeof(WaveLds<TILES>) / sizeof(float);   // of waves
-            park(at + wave * kStride);
-            __syncthreads();
-            float *out = p.partials + ((int64_t)b * kProductWaves + tau) * n;
-            int thread = threadIdx.x;
-            asm volatile("" : "+v"(thread));
-            const int32_t row = thread / 16, col = thread % 16;
-            if (!kPacked || (row < p.R && col < p.R)) {
-#pragma unroll
-                for (int i = 0; i < NT; ++i)
-#pragma unroll
-                    for (int j = kOne ? i : 0; j < NT; ++j) {
-                        double s = 0.0;
-                        for (int w = 0; w < kProductWaves; ++w)
-                            for (int g = 0; g < stretches; ++g)
-                                s += at[w * kStride + (i * NT + j) * 256 + (g * p.R + row) * 16 + g * p.R + col];
-                        put(out, false, (I * NT + i) * 16 + row, (J * NT + j) * 16 + col, (float)s);
-                    }
-            }
-            __syncthreads();
-            continue;
-        }
-        if (c0 >= p.P) continue;
-        // From here on elements are counted from c0, in 32 bits (scalar ones: an int64 compare takes
-        // vector instructions).  64 boundaries at a time, lane i that of tensor from + i.
-        auto boundary = [&](int32_t i) { return boundary_from(p.off[i + lane < p.T ? i + lane : p.T], c0); };
-        bound = boundary_from(edge, c0);
-        for (;;) {                     // the last tensor that begins by c0
-            tau = from + begun(bound, from, p.T);
-            if (tau < from + 62) break;
-            from = tau;
-            bound = boundary(from);
-            if (__builtin_amdgcn_readlane(bound, 1) > 0) break;
-        }
-        const int32_t span = (int32_t)super, size = (int32_t)(c1 - c0);
-        bool open = false;             // acc holds something of tensor tau
-        for (int32_t at = 0; at < size;) {
-            const int32_t next = at + span < size ? at + span : size;
+    const int64_t c = (int64_t)b * kProductWaves + wave;           // this wave's chunk
+    const int64_t b0 = (int64_t)b * kProductWaves * p.chunk, b1 = b0 + kProductWaves * p.chunk;
+    const int64_t c0 = c * p.chunk, c1 = c0 + p.chunk < p.P ? c0 + p.chunk : p.P;
+    int64_t s0 = c0;
+    a.template load<false>(s0 / kElems + fetched, p.P);
+    if (!kOne) o.template load<false>(s0 / kElems + fetched, p.P);
+    int32_t from;                  // lane i: where tensor from + i begins
+    int64_t edge = offsets_near(p.off, p.T, b0, &from);
+    clear();
+    int32_t bound = boundary_from(edge, b0), tau = from + begun(bound, from, p.T);
+    if (__builtin_amdgcn_readlane(bound, tau - from) <= 0 && __builtin_amdgcn_readlane(bound, tau - from + 1) >= b1 - b0 &&
+        b1 <= p.P) {
+        while (s0 < c1) {
             a.stash(mine, 0);
             if (!kOne) o.stash(mine, NT);
-            if (next < size) {
-                a.template load<false>((c0 + next) / kElems + fetched, p.P);
-                if (!kOne) o.template load<false>((c0 + next) / kElems + fetched, p.P);
+            s0 += super;
+            if (s0 < c1) {      // (on their way while these are multiplied)
+                a.template load<true>(s0 / kElems + fetched, p.P);
+                if (!kOne) o.template load<true>(s0 / kElems + fetched, p.P);
             }
-            while (tau < p.T) {
-                if (tau - from == 63) {
-                    from = tau;
-                    bound = boundary(from);
-                }
-                const int32_t begin = __builtin_amdgcn_readlane(bound, tau - from);
-                const int32_t end = __builtin_amdgcn_readlane(bound, tau - from + 1);
-                if (begin >= next) break;
-                if (end <= begin) {          // past the empty ones among the 64
-                    const uint64_t more = __ballot(bound > begin) & ~((uint64_t(2) << (tau - from)) - 1);
-                    tau = more ? from + __ffsll((unsigned long long)more) - 2 : from + 63;
-                    continue;
-                }
-                const int32_t lo = begin > at ? begin : at, hi = end < next ? end : next;
-                if (hi > lo) {
-                    open = true;
-                    if (hi - lo == span) {
-                        multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
-                    } else {
-                        // what of this lane's row is the tensor's
-                        const int first = at + held * kElems, f = lo - first, t = hi - first;
-                        const int unit0 = (lo - at) / Masks<F>::kUnit, units = (hi - at - 1) / Masks<F>::kUnit - unit0 + 1;
-                        multiply_super<F, NT, kOne, true>(mine, masks, f < 0 ? 0 : f, t > kElems ? kElems : t, unit0, units, acc);
-                    }
-                }
-                if (end > next) break;
-                if (open) {
-                    if (begin >= 0) leave(p.out + tau * n, true);        // (all of it was here)
-                    else leave(p.partials + (c + tau) * n, false);
-                    clear();
-                    open = false;
-                }
-                ++tau;
-            }
-            at = next;
+            multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
         }
-        if (open) leave(p.partials + (c + tau) * n, false);
+        float *at = kPacked ? parts : reinterpret_cast<float *>(shared);
+        constexpr int kStride = kPacked ? 256 : sizeof(WaveLds<TILES>) / sizeof(float);   // of waves
+        park(at + wave * kStride);
+        __syncthreads();
+        float *out = p.partials + ((int64_t)b * kProductWaves + tau) * n;
+        int thread = threadIdx.x;
+        asm volatile("" : "+v"(thread));
+        const int32_t row = thread / 16, col = thread % 16;
+        if (!kPacked || (row < p.R && col < p.R)) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = kOne ? i : 0; j < NT; ++j) {
+                    double s = 0.0;
+                    for (int w = 0; w < kProductWaves; ++w)
+                        for (int g = 0; g < stretches; ++g)
+                            s += at[w * kStride + (i * NT + j) * 256 + (g * p.R + row) * 16 + g * p.R + col];
+                    put(out, false, (I * NT + i) * 16 + row, (J * NT + j) * 16 + col, (float)s);
+                }
+        }
+        return;
     }
+    if (c0 >= p.P) return;
+    // From here on elements are counted from c0, in 32 bits (scalar ones: an int64 compare takes
+    // vector instructions).  64 boundaries at a time, lane i that of tensor from + i.
+    auto boundary = [&](int32_t i) { return boundary_from(p.off[i + lane < p.T ? i + lane : p.T], c0); };
+    bound = boundary_from(edge, c0);
+    for (;;) {                     // the last tensor that begins by c0
+        tau = from + begun(bound, from, p.T);
+        if (tau < from + 62) break;
+        from = tau;
+        bound = boundary(from);
+        if (__builtin_amdgcn_readlane(bound, 1) > 0) break;
+    }
+    const int32_t span = (int32_t)super, size = (int32_t)(c1 - c0);
+    bool open = false;             // acc holds something of tensor tau
+    for (int32_t at = 0; at < size;) {
+        const int32_t next = at + span < size ? at + span : size;
+        a.stash(mine, 0);
+        if (!kOne) o.stash(mine, NT);
+        if (next < size) {
+            a.template load<false>((c0 + next) / kElems + fetched, p.P);
+            if (!kOne) o.template load<false>((c0 + next) / kElems + fetched, p.P);
+        }
+        while (tau < p.T) {
+            if (tau - from == 63) {
+                from = tau;
+                bound = boundary(from);
+            }
+            const int32_t begin = __builtin_amdgcn_readlane(bound, tau - from);
+            const int32_t end = __builtin_amdgcn_readlane(bound, tau - from + 1);
+            if (begin >= next) break;
+            if (end <= begin) {          // past the empty ones among the 64
+                const uint64_t more = __ballot(bound > begin) & ~((uint64_t(2) << (tau - from)) - 1);
+                tau = more ? from + __ffsll((unsigned long long)more) - 2 : from + 63;
+                continue;
+            }
+            const int32_t lo = begin > at ? begin : at, hi = end < next ? end : next;
+            if (hi > lo) {
+                open = true;
+                if (hi - lo == span) {
+                    multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
+                } else {
+                    // what of this lane's row is the tensor's
+                    const int first = at + held * kElems, f = lo - first, t = hi - first;
+                    const int unit0 = (lo - at) / Masks<F>::kUnit, units = (hi - at - 1) / Masks<F>::kUnit - unit0 + 1;
+                    multiply_super<F, NT, kOne, true>(mine, masks, f < 0 ? 0 : f, t > kElems ? kElems : t, unit0, units, acc);
+                }
+            }
+            if (end > next) break;
+            if (open) {
+                if (begin >= 0) leave(p.out + tau * n, true);        // (all of it was here)
+                else leave(p.partials + (c + tau) * n, false);
+                clear();
+                open = false;
+            }
+            ++tau;
+        }
+        at = next;
+    }
+    if (open) leave(p.partials + (c + tau) * n, false);
 }
 
 // The tensors' sums of the partial sums that k_mx_product left, in 64 bits, by
@@ -1372,32 +1370,34 @@ extern "C" size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T) {
 
 namespace {
 
-// Groups of rows by K: the more a wave holds, the fewer times the rows are loaded,
-// but the fewer waves a CU holds.  us, E2M1, b is a: K = 64, P = 5M 112 as two groups
-// of 32, 78 as one of 64; K = 33, P = 20M 179, 103 as one of 64, 91 as one of 48; but
-// K = 100, P = 0.5M 53 as groups of 32, 62 of 48 and 60 of 64.  Two operands (twice
-// the registers): K = 33, P = 5M 76 as groups of 32, 52 as one of 48; K = 100, P = 5M
-// 393 as four of 32, 301 as three of 48; K = 64 130 as two of 32, 144 as two of 48.
+// Groups of rows by K: the more a wave holds, the fewer times the rows are loaded, but
+// the fewer waves a compute unit holds.  us, E2M1, b is a: K = 64, P = 5M 112 as groups of
+// 32, 78 as one of 64; K = 33, P = 20M 103 as one of 64, 91 as one of 48; K = 100 as
+// groups of 32 and of 48 P = 5M 152 and 137, P = 0.5M 32 and 39; K = 256 P = 4M 408 and 359,
+// P = 0.5M 69 and 75.  Two operands: K = 40, P = 5M 65 as groups of 32, 52 as one of 48;
+// K = 70 132 as nine pairs of 32, 119 as four of 48; K = 64 130 as two groups of 32, 144
+// as two of 48.
+template <int F, int NT, int Pairs>
+void launch_product(ProductParams &p, uint32_t pairs, hipStream_t st) {
+    p.pairs = pairs;
+    k_mx_product<F, NT, Pairs><<<(p.blocks + 7) / 8 * 8 * pairs, kThreads, 0, st>>>(p);
+}
+
 template <int F>
-void launch_product(const ProductParams &p, bool same, hipStream_t st) {
-    const uint32_t x = grid_for(p.blocks);
+void launch_product(ProductParams &p, bool same, hipStream_t st) {
     const uint32_t by32 = (p.K + 31) / 32, by48 = (p.K + 47) / 48;
     if (!same) {
-        if (p.K <= 16) k_mx_product<F, 1, kEvery><<<x, kThreads, 0, st>>>(p);
-        else if (by48 < by32) k_mx_product<F, 3, kEvery><<<dim3(x, by48 * by48), kThreads, 0, st>>>(p);
-        else k_mx_product<F, 2, kEvery><<<dim3(x, by32 * by32), kThreads, 0, st>>>(p);
+        if (p.K <= 16) launch_product<F, 1, kEvery>(p, 1, st);
+        else if (by48 < by32) launch_product<F, 3, kEvery>(p, by48 * by48, st);
+        else launch_product<F, 2, kEvery>(p, by32 * by32, st);
         return;
     }
-    if (p.K <= 16) {
-        k_mx_product<F, 1, kDiagonal><<<x, kThreads, 0, st>>>(p);
-    } else if (p.K <= 32 || p.K > 64) {
-        k_mx_product<F, 2, kDiagonal><<<dim3(x, by32), kThreads, 0, st>>>(p);
-        if (by32 > 1) k_mx_product<F, 2, kAbove><<<dim3(x, by32 * (by32 - 1) / 2), kThreads, 0, st>>>(p);
-    } else if (p.K <= 48) {
-        k_mx_product<F, 3, kDiagonal><<<x, kThreads, 0, st>>>(p);
-    } else {
-        k_mx_product<F, 4, kDiagonal><<<x, kThreads, 0, st>>>(p);
-    }
+    if (p.K <= 16) launch_product<F, 1, kOneGroup>(p, 1, st);
+    else if (p.K <= 32) launch_product<F, 2, kOneGroup>(p, 1, st);
+    else if (p.K <= 48) launch_product<F, 3, kOneGroup>(p, 1, st);
+    else if (p.K <= 64) launch_product<F, 4, kOneGroup>(p, 1, st);
+    else if (long_rows(p.P)) launch_product<F, 3, kUpper>(p, by48 * (by48 + 1) / 2, st);
+    else launch_product<F, 2, kUpper>(p, by32 * (by32 + 1) / 2, st);
 }
 
 }  // namespace

@@ -304,7 +304,7 @@ def _product_tol(off, mag):
 PRODUCT = [(1, 1, "one"), (2, 31, "empty"), (3, 33, "ones"), (8, 1025, "edges"), (16, 4099, "edges"), (17, 20_000, "many"),
            (32, 9000, "many"), (33, 2000, "ones"), (48, 30_000, "many"), (49, 3000, "many"), (64, 3000, "edges"), (65, 2500, "many"),
            (96, 20_000, "edges"), (130, 1500, "empty"), (100, 777, "many"),
-           (256, 600, "empty"), (4, 70_000, "empty"), (8, 300_007, "one"), (2, 4_300_007, "many"), (5, 2_000_000, "one"),
+           (256, 600, "empty"), (80, 40_000, "many"), (256, 9000, "edges"), (4, 70_000, "empty"), (8, 300_007, "one"), (2, 4_300_007, "many"), (5, 2_000_000, "one"),
            (4, 5000, "gaps"), (20, 40_000, "gaps"), (40, 5000, "gaps"),
            # stretches that share a tile
            (1, 4_400_000, "edges"), (3, 1_100_000, "many"), (4, 1_050_000, "gaps"), (7, 700_003, "many"), (8, 600_000, "edges"),
@@ -332,6 +332,29 @@ def test_product(A, fmt, K, P, cuts):
     other = _rows(A, codes2, byte2, P, fmt, pad=False)
     got = A.mx_product(rows, offd, other).cpu().numpy().astype(np.float64)
     assert np.all(np.abs(got - want) <= _product_tol(off, mag))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("K", [66, 97])
+def test_product_of_many_workers_and_long_rows(A, fmt, K):
+    """Against 64-bit products of what mx_dequantize reads, itself tested for every code and scale."""
+    P = (1 << 22) + 77
+    _say(f"product {fmt} K={K} P={P}")
+    torch.manual_seed(K)
+    x = torch.randn((K, P), device="cuda")
+    rows = A.mx_quantize(x, format=fmt)
+    v = A.mx_dequantize(rows, out=x)
+    off = np.array([0, 1, 5000, 5000, 70_001, 2_500_000, P - 3, P])
+    got = A.mx_product(rows, torch.from_numpy(off).cuda()).cpu().numpy().astype(np.float64)
+    for t, (lo, hi) in enumerate(zip(off[:-1], off[1:])):
+        want, mag = torch.zeros((2, K, K), dtype=torch.float64, device="cuda")
+        for at in range(lo, hi, 1 << 19):
+            d = v[:, at:min(at + (1 << 19), hi)].double()
+            want += d @ d.t().contiguous()
+            mag += d.abs() @ d.abs().t().contiguous()
+        tol = _product_tol(np.array([lo, hi]), mag.cpu().numpy()[None])[0]
+        assert np.all(np.abs(got[t] - want.cpu().numpy()) <= tol)
+    assert np.array_equal(got, got.transpose(0, 2, 1))
 
 
 @pytest.mark.parametrize("K", [1, 3, 8, 16, 20, 40, 60, 70])
