@@ -93,11 +93,15 @@ def _matrix(t: torch.Tensor, K: int, P: int, dev: int, name: str) -> int:
     """Row stride of a float32 [K, P] tensor."""
     if t.dtype is not _F32 or t.shape != (K, P) or t.get_device() != dev:
         raise ValueError(f"{name} must be float32 [{K}, {P}] on device {dev}")
-    if P > 1 and t.stride(1) != 1:
+    return _row_stride(t, K, P, name)
+
+
+def _row_stride(t: torch.Tensor, K: int, P: int, name: str) -> int:
+    ld, one = t.stride()
+    if one != 1 and P > 1:
         raise ValueError(f"{name} must have contiguous rows")
     if K == 1:
         return P
-    ld = t.stride(0)
     if ld < P:
         raise ValueError(f"{name} must have rows that do not overlap")
     return ld
@@ -126,10 +130,10 @@ def mx_quantize(x: torch.Tensor, base: Optional[torch.Tensor] = None, residual: 
     written to residual_out, by default to residual itself, and not kept where both are None.
     out: rows to write (their format is the one used)."""
     dev = x.get_device()
-    if x.dim() != 2 or dev < 0:
+    if x.dtype is not _F32 or x.dim() != 2 or dev < 0:
         raise ValueError("x must be a float32 matrix on a GPU")
     K, P = x.shape
-    x_ld = _matrix(x, K, P, dev, "x")
+    x_ld = _row_stride(x, K, P, "x")
     base_ptr = _vector(base, P, dev, "base")
     r_in = r_out = None
     r_ld = 0
