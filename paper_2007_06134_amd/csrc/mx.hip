@@ -1358,8 +1358,10 @@ extern "C" int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
         else launch_average<ADPSGD_MX_E4M3>(p, st);
         if (int rc = launched("average launch")) return rc;
     }
-    k_mx_variance<<<grid_for((uint64_t)T), p.chunks > 4096 ? 1024 : kThreads, 0, st>>>(tensor_offsets, p.partials, chunk, P, T,
-                                                              (double)rows->K * rows->K, var);
+    // more threads where a tensor may have many partial sums (a launch has less than 2^32 threads)
+    const int threads = p.chunks > 4096 && T < 1 << 16 ? 1024 : kThreads;
+    k_mx_variance<<<grid_for((uint64_t)T), threads, 0, st>>>(tensor_offsets, p.partials, chunk, P, T,
+                                                             (double)rows->K * rows->K, var);
     return launched("variance launch");
 }
 

@@ -425,6 +425,28 @@ def test_no_parameters(A, fmt):
     assert A.mx_product(rows, off).abs().max().item() == 0
 
 
+def test_as_many_tensors_as_a_call_takes(A):
+    """2^24 tensors, of one element each but the last: every kernel's grid still fits a launch."""
+    K, T = 2, 1 << 24
+    P = T + 1000
+    torch.manual_seed(5)
+    rows = A.mx_quantize(torch.randn((K, P), device="cuda"))
+    off = torch.arange(T + 1, device="cuda")
+    off[T] = P
+    _say(f"T={T}")
+    v = A.mx_dequantize(rows).double()
+    d = (v - v.mean(0)).square().sum(0) / K
+    want = torch.cat((d[:T - 1], d[T - 1:].sum()[None]))
+    _, var = A.mx_average(rows, off)
+    assert bool(((var - want).abs() <= 1e-12 * want).all())
+    c = A.mx_product(rows, off)
+    # (single products are exact in fp32; the last tensor's are up to 32 sums of 32 each)
+    assert torch.equal(c[:T - 1, 0, 1].double(), (v[0] * v[1])[:T - 1]) and torch.equal(c[:, 0, 1], c[:, 1, 0])
+    assert torch.equal(c[:T - 1, 1, 1].double(), v[1, :T - 1].square())
+    mag = (v[0] * v[1])[T - 1:].abs().sum()
+    assert bool((c[T - 1, 0, 1].double() - (v[0] * v[1])[T - 1:].sum()).abs() <= (4 * 32 + 8) * 2.0 ** -24 * mag)
+
+
 def test_offsets_that_do_not_fit_touch_nothing_else(A):
     """The offsets are read on the device only: boundaries past P, before 0 or out of order leave the
     model right and every other byte as it was."""
