@@ -110,7 +110,7 @@ def _row_stride(t: torch.Tensor, K: int, P: int, name: str) -> int:
 def _vector(t: Optional[torch.Tensor], P: int, dev: int, name: str) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype is not _F32 or t.shape != (P,) or t.get_device() != dev or (P > 1 and t.stride(0) != 1):
+    if t.dtype is not _F32 or t.dim() != 1 or t.numel() != P or t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous float32 [{P}] on device {dev}")
     return t.data_ptr()
 
