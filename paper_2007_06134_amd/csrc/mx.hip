@@ -1455,8 +1455,7 @@ extern "C" int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *
     const int64_t n = (int64_t)a->K * a->K, items = (int64_t)p.blocks * kProductWaves / T;
     int32_t outs = 1, share = 1;
     while (outs < (items > 16 ? 16 : 128) && outs < n) outs *= 2;
-    while (share < 1024 / std::min(outs, 64) && share * 8 < items) share *= 2;
-    while (outs * share > 1024) outs /= 2;
+    while (outs * share < 1024 && share * 8 < items) share *= 2;
     const uint32_t threads = (uint32_t)(outs * share);
     k_mx_product_sum<<<dim3(grid_for((uint64_t)T), (uint32_t)((n + outs - 1) / outs)), threads, 0, st>>>(
         tensor_offsets, p.partials, p.chunk, P, a->K, T, same, outs, out);
