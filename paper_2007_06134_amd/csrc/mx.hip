@@ -775,8 +775,8 @@ enum { kOneGroup = 0, kUpper = 1, kEvery = 2 };
 //
 // NT: tiles of 16 rows of an operand that a wave holds at once (of one group, those
 // below the diagonal are left out).  The pairs of groups of the same elements follow each
-// other on one XCD, whose L2 gives the rows to all but the first (K = 256, P = 4M 767 ->
-// 430 us; two sets of 128, P = 5M 359 -> 230).
+// other on one XCD, whose L2 gives the rows to all but the first (K = 256, P = 4M 430 us,
+// 767 with the pairs apart; two sets of 128, P = 5M 230 and 359).
 template <int F, int NT, int Pairs>
 __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     constexpr bool kOne = Pairs == kOneGroup;
@@ -1170,15 +1170,15 @@ int32_t tile_workers(int32_t K, int64_t P) {
 }
 
 // Elements of a product's wave: of as many waves as the compute units hold evenly, four to
-// a block and 256 blocks a step.  20 waves a unit of the kernels for up to 16 workers
-// (K = 8, P = 138M: 106 us; 108 with 32, 115 with 16; K = 16, P = 25.6M, 8 bits: 86, 91
-// and 89), 8 for up to 32 (K = 24, P = 5M: 29 us; 36 with 13, 31 with 12, 27 with 4, but
-// K = 32, P = 20M 78 with 8 and 92 with 4), 4 for up to 64 (K = 64, P = 5M: 55 us; 66
-// with 2; two sets of 40, P = 10M, 8 bits: 160, and 197 with 5), and a whole number of
-// fours where more are needed (two sets of 40, P = 20M: 161 us with 8, 203 with 5).
-// More workers fill the units with pairs of groups: fewer waves, so that the K x K
-// partial sums come to 8 MB at most.  No wave takes less than its partial sums outweigh,
-// nor more than 16384 elements of a row (of which fp32 sums are taken).
+// a block and 256 blocks a step (us, with this many waves a unit).  20 of the kernels for
+// up to 16 workers (K = 8, P = 138M: 106; 108 with 32; K = 16, P = 25.6M, 8 bits: 87, 94
+// with 32, 92 with 16), 8 for up to 32 (K = 24, P = 5M: 24.8; 25.5 with 12, 28.3 with 13,
+// 26.4 with 4; K = 32, P = 20M: 73, 78 with 12, 85 with 13), 4 for up to 64 (K = 64, P =
+// 5M: 49; 58 with 2, 60 with 5, 57 with 8), and a whole number of fours where more are
+// needed (two sets of 40, P = 20M: 164 with 8, 209 with 5).  More workers fill the units
+// with pairs of groups: fewer waves, so that the K x K partial sums come to 8 MB at most.
+// No wave takes less than its partial sums outweigh, nor more than 16384 elements of a
+// row (of which fp32 sums are taken).
 int64_t product_chunk(int32_t K, int64_t P) {
     const int64_t super = kSuper * (16 / tile_workers(K, P)), most = 32;
     const int64_t supers = (P + super - 1) / super, least = (15 * (int64_t)K + super - 1) / super;
@@ -1373,12 +1373,12 @@ extern "C" size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T) {
 namespace {
 
 // Groups of rows by K: the more a wave holds, the fewer times the rows are loaded, but
-// the fewer waves a compute unit holds.  us, E2M1, b is a: K = 64, P = 5M 112 as groups of
-// 32, 78 as one of 64; K = 33, P = 20M 103 as one of 64, 91 as one of 48; K = 100 as
-// groups of 32 and of 48 P = 5M 152 and 137, P = 0.5M 32 and 39; K = 256 P = 4M 408 and 359,
-// P = 0.5M 69 and 75.  Two operands: K = 40, P = 5M 65 as groups of 32, 52 as one of 48;
-// K = 70 132 as nine pairs of 32, 119 as four of 48; K = 64 130 as two groups of 32, 144
-// as two of 48.
+// the fewer waves a compute unit holds.  us, E2M1, b is a: K = 64, P = 5M 67 as groups of
+// 32, 49 as one of 64; K = 33, P = 20M 140 as groups of 32, 84 as one of 64, 79 as one of
+// 48; K = 100 as groups of 32 and of 48 P = 5M 143 and 127, P = 0.5M 27 and 35; K = 256
+// P = 4.3M 435 and 379, P = 0.5M 69 and 75.  Two operands: K = 40, P = 5M 65 as groups of
+// 32, 52 as one of 48; K = 70 131 as nine pairs of 32, 118 as four of 48; K = 64 93 as
+// two groups of 32, 116 as two of 48.
 template <int F, int NT, int Pairs>
 void launch_product(ProductParams &p, uint32_t pairs, hipStream_t st) {
     p.pairs = pairs;
