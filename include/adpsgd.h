@@ -383,13 +383,13 @@ typedef struct {
     void *scales;
     int64_t code_stride;
     int64_t scale_stride;
-    int64_t P;           /* >= 0                                    */
+    int64_t P;           /* in [0, 2^34]                            */
     int32_t K;           /* in [1, 65536], K * P below 2^39         */
     int32_t format;      /* ADPSGD_MX_*                             */
 } adpsgd_mx_rows;
 
 /* Row strides (bytes) to use for P parameters: the least odd number of 256-byte
- * units that holds a row (0 for P <= 0 or an unknown format). */
+ * units that holds a row (0 for P <= 0, P > 2^34 or an unknown format). */
 ADPSGD_API int64_t adpsgd_mx_code_stride(int32_t format, int64_t P);
 ADPSGD_API int64_t adpsgd_mx_scale_stride(int64_t P);
 

@@ -34,6 +34,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMxBlock = 32;           // elements that share a scale
 constexpr int32_t kMaxK = 65536;
+constexpr int64_t kMaxP = int64_t(1) << 34;
 constexpr int32_t kMaxT = 1 << 24;
 constexpr int32_t kMaxProductK = 256;
 constexpr int64_t kMaxStride = int64_t(1) << 44;   // K rows of this many floats still have 63-bit addresses
@@ -1093,7 +1094,7 @@ int check_rows(const adpsgd_mx_rows *r, const char *name) {
     if (r->format != ADPSGD_MX_E2M1 && r->format != ADPSGD_MX_E4M3)
         return fail(ADPSGD_EINVAL, n + ".format must be ADPSGD_MX_E2M1 or ADPSGD_MX_E4M3");
     if (r->K < 1 || r->K > kMaxK) return fail(ADPSGD_EINVAL, "K must be in [1, 65536]");
-    if (r->P < 0 || (r->P + 3) / 4 > (int64_t(1) << 32)) return fail(ADPSGD_EINVAL, "P must be >= 0 with P/4 below 2^32");
+    if (r->P < 0 || r->P > kMaxP) return fail(ADPSGD_EINVAL, "P must be in [0, 2^34]");
     if ((r->P + kPiece - 1) / kPiece > kMaxPieces / r->K) return fail(ADPSGD_EINVAL, "K * P must be below 2^39");
     const Bytes need = row_bytes(r->format, r->P);
     if (r->code_stride < need.codes || r->code_stride % 16 != 0 || r->code_stride > kMaxStride)
@@ -1195,13 +1196,13 @@ int64_t product_blocks(int32_t K, int64_t P) {
 }  // namespace
 
 extern "C" int64_t adpsgd_mx_code_stride(int32_t format, int64_t P) {
-    if ((format != ADPSGD_MX_E2M1 && format != ADPSGD_MX_E4M3) || P <= 0) return 0;
+    if ((format != ADPSGD_MX_E2M1 && format != ADPSGD_MX_E4M3) || P <= 0 || P > kMaxP) return 0;
     const int64_t n = (row_bytes(format, P).codes + 255) / 256;
     return 256 * (n + 1 - n % 2);
 }
 
 extern "C" int64_t adpsgd_mx_scale_stride(int64_t P) {
-    if (P <= 0) return 0;
+    if (P <= 0 || P > kMaxP) return 0;
     const int64_t n = (row_bytes(ADPSGD_MX_E2M1, P).scales + 255) / 256;
     return 256 * (n + 1 - n % 2);
 }
@@ -1310,7 +1311,7 @@ extern "C" int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *bas
 }
 
 extern "C" size_t adpsgd_mx_average_workspace(int32_t K, int64_t P, int32_t T) {
-    if (K < 1 || K > kMaxK || P < 0 || (P + 3) / 4 > (int64_t(1) << 32) || T < 1 || T > kMaxT) return 0;
+    if (K < 1 || K > kMaxK || P < 0 || P > kMaxP || T < 1 || T > kMaxT) return 0;
     const int64_t chunk = average_chunk_elements(P);
     return sizeof(double) * (size_t)((P + chunk - 1) / chunk + T);
 }
@@ -1366,7 +1367,7 @@ extern "C" int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
 }
 
 extern "C" size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T) {
-    if (K < 1 || K > kMaxProductK || P < 0 || (P + 3) / 4 > (int64_t(1) << 32) || T < 1 || T > kMaxT) return 0;
+    if (K < 1 || K > kMaxProductK || P < 0 || P > kMaxP || T < 1 || T > kMaxT) return 0;
     return sizeof(float) * (size_t)(product_blocks(K, P) * kProductWaves + T) * K * K;
 }
 

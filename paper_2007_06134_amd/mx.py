@@ -67,6 +67,8 @@ class MxRows:
             raise ValueError("format must be MX_E2M1 or MX_E4M3")
         if K < 1 or P < 0:
             raise ValueError("K must be >= 1 and P >= 0")
+        if P > 1 << 34:
+            raise ValueError("P must be at most 2^34")
         return cls(torch.empty((K, lib.adpsgd_mx_code_stride(format, P)), dtype=_U8, device=device),
                    torch.empty((K, lib.adpsgd_mx_scale_stride(P)), dtype=_U8, device=device), P, format)
 

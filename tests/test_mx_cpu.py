@@ -66,6 +66,23 @@ def test_strides_whose_addresses_would_not_fit_are_refused(A, lib, K):
             assert call() == A.EINVAL and "2^44" in A.adpsgd_last_error()
 
 
+@pytest.mark.parametrize("P", [(1 << 34) + 1, (1 << 63) - 4, (1 << 63) - 1])
+def test_lengths_past_the_limit_are_refused(A, lib, P):
+    """Also those whose bytes or blocks no 64-bit count holds."""
+    r = C.byref(_rows(A, P=P, K=1, code_stride=1 << 43, scale_stride=1 << 43))
+    for call in (lambda: lib.adpsgd_mx_quantize(r, BASE, 0, None, None, None, 0, None),
+                 lambda: lib.adpsgd_mx_dequantize(r, None, BASE, 0, None),
+                 lambda: lib.adpsgd_mx_average(r, 1, BASE, None, BASE, None, 0, BASE, BASE, 1 << 60, None),
+                 lambda: lib.adpsgd_mx_product(r, None, 1, BASE, BASE, BASE, 1 << 60, None)):
+        assert call() == A.EINVAL and "P must" in A.adpsgd_last_error()
+    assert lib.adpsgd_mx_average_workspace(1, P, 1) == 0 and lib.adpsgd_mx_product_workspace(1, P, 1) == 0
+    for fmt in (A.MX_E2M1, A.MX_E4M3):
+        assert lib.adpsgd_mx_code_stride(fmt, P) == 0
+        with pytest.raises(ValueError):
+            A.MxRows.empty(1, P, fmt, device="cpu")
+    assert lib.adpsgd_mx_scale_stride(P) == 0
+
+
 def test_null_rows(A, lib):
     assert lib.adpsgd_mx_quantize(None, BASE, 0, None, None, None, 0, None) == A.EINVAL
     assert lib.adpsgd_mx_dequantize(None, None, BASE, 0, None) == A.EINVAL
