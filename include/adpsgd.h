@@ -432,10 +432,10 @@ ADPSGD_API int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
  * b_k,i of the rows of two sets of messages of the same format, K <= 256 and P
  * (b NULL or a itself: of one set with itself, a symmetric matrix; then
  * (tr C - 1'C1 / K) / K is adpsgd_mx_average's variance).  Sums of up to 16384
- * products are taken in fp32, the rest in 64 bits.  E4M3 elements below
- * 2^-126 are rounded to multiples of 2^-133.  tensor_offsets and workspace
- * (adpsgd_mx_product_workspace bytes) as above.  Both workspace functions
- * return 0 for invalid arguments. */
+ * products are taken in fp32 (E4M3: in two levels), the rest in 64 bits.  E4M3
+ * elements below 2^-126 are rounded to multiples of 2^-133.  tensor_offsets and
+ * workspace (adpsgd_mx_product_workspace bytes) as above.  Both workspace
+ * functions return 0 for invalid arguments. */
 ADPSGD_API size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T);
 ADPSGD_API int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *b, int32_t T,
                                  const int64_t *tensor_offsets, float *out, void *workspace, size_t workspace_bytes,

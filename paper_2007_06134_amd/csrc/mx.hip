@@ -813,6 +813,30 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
     };
+    // E4M3: two levels of fp32 sums, acc over 256 bytes of each row and total of those.  (Error
+    // against 64 bits at K = 16, P = 25.6M 3.1e-8 of the result; 5.5e-7 with one level.  K = 16 82 us
+    // either way, K = 32, P = 20M 128 and 125.  Sums of 4-bit products are mostly exact: 2.6e-8.)
+    constexpr bool kLevels = F == ADPSGD_MX_E4M3;
+    v4 total[kLevels ? NT : 1][kLevels ? NT : 1];
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int j = kOne ? i : 0; j < NT; ++j) f(i, j);
+    };
+    auto level = [&] {
+        if constexpr (kLevels) each([&](int i, int j) {
+            total[i][j] += acc[i][j];
+            acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
+        });
+    };
+    auto join = [&] {
+        if constexpr (kLevels) each([&](int i, int j) {
+            acc[i][j] = total[i][j];
+            total[i][j] = v4{0.f, 0.f, 0.f, 0.f};
+        });
+    };
+    if constexpr (kLevels) each([&](int i, int j) { total[i][j] = v4{0.f, 0.f, 0.f, 0.f}; });
     auto park = [&](float *at) {
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -889,7 +913,9 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
                 if (!kOne) o.template load<true>(s0 / kElems + fetched, p.P);
             }
             multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
+            level();
         }
+        join();
         float *at = kPacked ? parts : reinterpret_cast<float *>(shared);
         constexpr int kStride = kPacked ? 256 : sizeof(WaveLds<TILES>) / sizeof(float);   // of waves
         park(at + wave * kStride);
@@ -952,15 +978,18 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
                 open = true;
                 if (hi - lo == span) {
                     multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
+            level();
                 } else {
                     // what of this lane's row is the tensor's
                     const int first = at + held * kElems, f = lo - first, t = hi - first;
                     const int unit0 = (lo - at) / Masks<F>::kUnit, units = (hi - at - 1) / Masks<F>::kUnit - unit0 + 1;
                     multiply_super<F, NT, kOne, true>(mine, masks, f < 0 ? 0 : f, t > kElems ? kElems : t, unit0, units, acc);
+                        level();
                 }
             }
             if (end > next) break;
             if (open) {
+                join();
                 if (begin >= 0) leave(p.out + tau * n, true);        // (all of it was here)
                 else leave(p.partials + (c + tau) * n, false);
                 clear();
@@ -970,7 +999,10 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
         }
         at = next;
     }
-    if (open) leave(p.partials + (c + tau) * n, false);
+    if (open) {
+        join();
+        leave(p.partials + (c + tau) * n, false);
+    }
 }
 
 // The tensors' sums of the partial sums that k_mx_product left, in 64 bits, by

@@ -357,6 +357,20 @@ def test_product_of_many_workers_and_long_rows(A, fmt, K):
     assert np.array_equal(got, got.transpose(0, 2, 1))
 
 
+@pytest.mark.parametrize("K", [5, 16, 40, 70])
+def test_eight_bit_products_are_summed_in_two_levels(A, K):
+    """Positive elements, whose partial sums only grow: 8 matrix instructions a level of 256 elements, then
+    at most 64 of those sums, the joins in 64 bits and the result's rounding."""
+    P = 600_000
+    torch.manual_seed(K)
+    x = torch.rand((K, P), device="cuda") + 0.1
+    rows = A.mx_quantize(x, format=A.MX_E4M3)
+    v = A.mx_dequantize(rows).double()
+    got = A.mx_product(rows, torch.tensor([0, P], device="cuda"))[0].double()
+    want = v @ v.t().contiguous()
+    assert bool(((got - want).abs() <= (4 * 8 + 64 + 2) * 2.0 ** -24 * want).all())
+
+
 @pytest.mark.parametrize("K", [1, 3, 8, 16, 20, 40, 60, 70])
 def test_product_of_four_bit_messages_of_one_scale_is_exact(A, K):
     """E2M1 products are quarters of integers up to 144: sums of 16384 of them fit an fp32 mantissa."""
