@@ -86,8 +86,10 @@ class Adpsgd:
                                   xstar=self.xstar.data_ptr(), workspace=self.workspace.data_ptr(),
                                   workspace_bytes=nbytes, stream=self.stream.cuda_stream,
                                   row_stride=self.row_stride)
-        # the state of average_mx (made by its first call)
+        # the state of average_mx (made by its first call or by mx_begin).  _mx_lost: syncs of fp32
+        # replicas have moved the model that the workers share, and mx_base is not that model.
         self.mx_base = self.mx_residual = None
+        self._mx_lost = False
         self._mx_rows = self._mx_offsets = None
         with torch.cuda.device(self.device):
             self.ctx = adpsgd_init(self.K, self.P, off, hp, self.buf)
@@ -101,26 +103,52 @@ class Adpsgd:
         adpsgd_local_steps(self.ctx, n)
 
     def average(self) -> np.ndarray:
-        return adpsgd_average(self.ctx, self.T)
+        return self._following(adpsgd_average, lambda var: 1, self.T)
 
     def step_average(self) -> np.ndarray:
-        return adpsgd_step_average(self.ctx, self.T)
+        return self._following(adpsgd_step_average, lambda var: 1, self.T)
+
+    def _following(self, call, syncs, *args, **kw):
+        """call(self.ctx, ...), which synchronizes fp32 replicas syncs(result) times.  Where it ends with
+        such a sync mx_base follows (if average_mx is in use), else it is lost."""
+        try:
+            out = call(self.ctx, *args, **kw)
+        except (TypeError, ValueError):
+            raise                              # (of arguments: nothing ran)
+        except BaseException as e:
+            if getattr(e, "code", None) != EINVAL:
+                self._mx_lost = True
+            raise
+        if syncs(out):
+            self._mx_lost = True
+            if self.mx_base is not None and self.get_state().cnt == 0:
+                self.mx_begin()
+        return out
 
     def average_mx(self, format: int = MX_E2M1, error_feedback: bool = True, products: bool = False):
         """The synchronization with microscaled messages in place of fp32 replicas: every worker sends
-        its difference from mx_base, the model after the last such sync (0 at first, as the replicas),
+        its difference from mx_base, the model after the last sync (0 at first, as the replicas),
         in `format`; all replicas become mx_base + the mean of what was sent, which is the new mx_base.
-        With error_feedback what a worker's message left out (mx_residual) is added to its next one.
+        With error_feedback what a worker's message left out (mx_residual) is added to its next one;
+        a sync of fp32 replicas ends what is owed.
 
         Returns the per-tensor variances of what was sent, for ``schedule`` (and, with products, the
         workers' inner products [T, K, K] as ``mx_product`` gives them).  Like ``average`` it restarts
         the counter and waits for the stream; momentum stays local (with avg_momentum it is refused).
-        mx_base and mx_residual belong to a checkpoint, next to x and m; reset() zeroes them."""
+
+        Syncs of fp32 replicas may come between: mx_base follows ``average``, ``step_average`` and a run that
+        ends with a sync.  Where it could not follow (those calls, or the state of another run, before the first
+        of this one; a run that stepped on past its last sync) the call is refused until ``mx_begin`` names a
+        base: a message would be most of a model in a few bits.  mx_base and mx_residual belong to a
+        checkpoint, next to x and m (``mx_begin`` takes them back); reset() zeroes them."""
         torch = self.torch
         if self.hp.avg_momentum:
             raise ValueError("average_mx keeps the momentum local; the hyper-parameters ask for avg_momentum")
         if products and self.K > 256:      # (before anything is sent)
             raise ValueError("products are for at most 256 workers")
+        if self._mx_lost:
+            raise AdpsgdError(ESTATE, "the workers' shared model has moved past mx_base: call mx_begin right behind a "
+                                      "sync, or with the model after the last one")
         with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
             if self.mx_base is None:
                 self.mx_base = torch.zeros((self.P,), device=self.device)
@@ -141,17 +169,46 @@ class Adpsgd:
                 out = (out, c.cpu().numpy())
         return out
 
+    def mx_begin(self, base=None, residual=None) -> None:
+        """Sets what the next ``average_mx`` starts from: mx_base to base [P], the model that all workers know,
+        and mx_residual to residual [K, P], what each one's messages still owe (zero by default).  float32
+        tensors on any device, copied.  Without a base it is what the replicas hold now: right behind a sync
+        of fp32 replicas, or where every row of x was just given the model to start from."""
+        torch = self.torch
+        for name, t, shape in (("base", base, (self.P,)), ("residual", residual, (self.K, self.P))):
+            if t is not None and (t.dtype is not torch.float32 or t.shape != shape):
+                raise ValueError(f"{name} must be float32 {list(shape)}")
+        if base is None and self.get_state().cnt != 0:
+            raise ValueError("the workers have stepped on since the last sync: base must be given")
+        self.stream.wait_stream(torch.cuda.current_stream(self.device))
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream), torch.no_grad():
+            to_base, to_residual = self.mx_base, self.mx_residual
+            if to_base is None:
+                to_base = torch.empty((self.P,), device=self.device, dtype=torch.float32)
+            if to_residual is None and residual is not None:
+                to_residual = torch.empty_like(self._x_rows)[:, :self.P]
+            to_base.copy_(self.x[0] if base is None else base)
+            if residual is not None:
+                to_residual.copy_(residual)
+            elif to_residual is not None:
+                to_residual.zero_()
+            for t in (base, residual):         # (the caller may drop them before the copies have run)
+                if t is not None and t.is_cuda:
+                    t.record_stream(self.stream)
+        self.mx_base, self.mx_residual, self._mx_lost = to_base, to_residual, False
+
     def schedule(self, var: np.ndarray) -> int:
         return adpsgd_schedule(self.ctx, var)
 
     def run(self, n_steps: int, log_cap: Optional[int] = None, with_var: bool = True):
-        return adpsgd_run(self.ctx, n_steps, self.T, log_cap=log_cap, with_var=with_var)
+        return self._following(adpsgd_run, lambda out: out[2], n_steps, self.T, log_cap=log_cap, with_var=with_var)
 
     def run_traced(self, n_steps: int, log_cap: Optional[int] = None, with_var: bool = True):
-        return adpsgd_run_traced(self.ctx, n_steps, self.T, log_cap=log_cap, with_var=with_var)
+        return self._following(adpsgd_run_traced, lambda out: out[2], n_steps, self.T, log_cap=log_cap, with_var=with_var)
 
     def reset(self) -> None:
         adpsgd_reset(self.ctx)
+        self._mx_lost = False
         with self.torch.cuda.stream(self.stream):
             for t in (self.mx_base, self.mx_residual):
                 if t is not None:
@@ -162,7 +219,10 @@ class Adpsgd:
         return adpsgd_get_state(self.ctx)
 
     def set_state(self, st: adpsgd_state) -> None:
+        t = self.get_state().t
         adpsgd_set_state(self.ctx, st)
+        if st.t != t and self.mx_base is None:     # (another run's replicas, whose last sync is not known here)
+            self._mx_lost = True
 
     @property
     def step_launch(self) -> tuple:
