@@ -130,7 +130,7 @@ class Adpsgd:
         its difference from mx_base, the model after the last sync (0 at first, as the replicas),
         in `format`; all replicas become mx_base + the mean of what was sent, which is the new mx_base.
         With error_feedback what a worker's message left out (mx_residual) is added to its next one;
-        a sync of fp32 replicas ends what is owed.
+        a message without it, and a sync of fp32 replicas, end what is owed.
 
         Returns the per-tensor variances of what was sent, for ``schedule`` (and, with products, the
         workers' inner products [T, K, K] as ``mx_product`` gives them).  Like ``average`` it restarts
@@ -158,6 +158,8 @@ class Adpsgd:
                 self._mx_rows = MxRows.empty(self.K, self.P, format, self.device)
             if self._mx_offsets is None:
                 self._mx_offsets = torch.from_numpy(self.offsets).to(self.device)
+            if not error_feedback and self.mx_residual is not None:
+                self.mx_residual.zero_()
             st = self.get_state()
             st.cnt = 0
             self.set_state(st)

@@ -147,6 +147,22 @@ def test_a_run_that_stops_at_a_sum_that_is_not_finite(A):
             eng.average_mx()
 
 
+def test_errors_are_not_carried_past_a_message_without_feedback(A):
+    w = _const(K=4)
+    zero = np.zeros((w.K, w.P), np.float32)
+    with A.Adpsgd.from_workload(w) as eng:
+        eng.local_steps(4)
+        left = _sync_is_of(A, eng, w, np.zeros(w.P, np.float32), zero)
+        assert left.any()
+        base = eng.mx_base.cpu().numpy()
+        eng.local_steps(4)
+        _sync_is_of(A, eng, w, base, None, feedback=False)
+        assert not eng.mx_residual.any()
+        base = eng.mx_base.cpu().numpy()
+        eng.local_steps(4)
+        _sync_is_of(A, eng, w, base, zero)
+
+
 @pytest.mark.parametrize("where", ["cpu", "cuda", "stream"])
 def test_resumes_bit_exactly_from_mx_begin(A, where):
     """A checkpoint of x, m, the controller, mx_base and mx_residual into a new engine."""
