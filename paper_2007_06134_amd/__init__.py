@@ -22,6 +22,7 @@ from ._native import (  # noqa: F401
     adpsgd_padded_row_stride, adpsgd_state, adpsgd_step_average, adpsgd_sync_rec, adpsgd_timing,
     adpsgd_workspace_bytes, make_hparams,
 )
+from . import mx as _mx
 from .mx import MxRows, mx_average, mx_dequantize, mx_product, mx_quantize  # noqa: F401
 
 
@@ -158,14 +159,18 @@ class Adpsgd:
                 self._mx_rows = MxRows.empty(self.K, self.P, format, self.device)
             if self._mx_offsets is None:
                 self._mx_offsets = torch.from_numpy(self.offsets).to(self.device)
+            # (all memory before anything is sent, so that a call that fails has moved nothing)
+            rows, off = self._mx_rows, self._mx_offsets
+            made = _mx.average_buffers(rows, self.T, off)
+            made_c = _mx.product_buffers(rows, self.T, off) if products else None
+            mx_quantize(self.x, self.mx_base, self.mx_residual if error_feedback else None, out=rows)
             if not error_feedback and self.mx_residual is not None:
                 self.mx_residual.zero_()
+            c = mx_product(rows, off, _buffers=made_c) if products else None
+            _, var = mx_average(rows, off, self.mx_base, x=self.x, base_out=self.mx_base, _buffers=made)
             st = self.get_state()
             st.cnt = 0
             self.set_state(st)
-            rows = mx_quantize(self.x, self.mx_base, self.mx_residual if error_feedback else None, out=self._mx_rows)
-            c = mx_product(rows, self._mx_offsets) if products else None
-            _, var = mx_average(rows, self._mx_offsets, self.mx_base, x=self.x, base_out=self.mx_base)
             out = var.cpu().numpy()
             if c is not None:
                 out = (out, c.cpu().numpy())

@@ -168,9 +168,21 @@ def mx_dequantize(rows: MxRows, base: Optional[torch.Tensor] = None, *,
     return out
 
 
+# A call's output of sums, its workspace and the workspace's bytes: for T tensors, where the offsets are.  The
+# engine makes them before it sends anything and hands them to the call (_buffers).
+def average_buffers(rows: MxRows, T: int, offsets: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor, int]:
+    need = lib.adpsgd_mx_average_workspace(rows._K, rows._P, T)
+    return offsets.new_empty(T, dtype=_F64), offsets.new_empty(need + 7 >> 3), need
+
+
+def product_buffers(a: MxRows, T: int, offsets: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor, int]:
+    need = lib.adpsgd_mx_product_workspace(a._K, a._P, T)
+    return offsets.new_empty((T, a._K, a._K), dtype=_F32), offsets.new_empty(need + 7 >> 3), need
+
+
 def mx_average(rows: MxRows, offsets: torch.Tensor, base: Optional[torch.Tensor] = None, *,
-               x: Optional[torch.Tensor] = None,
-               base_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+               x: Optional[torch.Tensor] = None, base_out: Optional[torch.Tensor] = None,
+               _buffers: Optional[tuple] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The synchronization: (base + the rows' mean, float32 [P]; every tensor's variance, float64 [T]).
 
     offsets: int64 [T + 1] on the device, the tensors' boundaries as for ``Adpsgd`` (0 first, P last;
@@ -185,24 +197,21 @@ def mx_average(rows: MxRows, offsets: torch.Tensor, base: Optional[torch.Tensor]
     if base_out is None:
         base_out = torch.empty((P,), dtype=_F32, device=rows._codes.device)
     out_ptr = _vector(base_out, P, dev, "base_out")
-    var = offsets.new_empty(T, dtype=_F64)
-    need = lib.adpsgd_mx_average_workspace(K, P, T)
-    work = offsets.new_empty(need + 7 >> 3)
+    var, work, need = _buffers or average_buffers(rows, T, offsets)
     _run(lib.adpsgd_mx_average, dev, rows._ref, T, offsets.data_ptr(), base_ptr, out_ptr, x_ptr, x_ld, var.data_ptr(),
          work.data_ptr(), need)
     return base_out, var
 
 
-def mx_product(a: MxRows, offsets: torch.Tensor, b: Optional[MxRows] = None) -> torch.Tensor:
+def mx_product(a: MxRows, offsets: torch.Tensor, b: Optional[MxRows] = None, *,
+               _buffers: Optional[tuple] = None) -> torch.Tensor:
     """Inner products of the rows of a with those of b (of a, where b is None) for every tensor:
     float32 [T, K, K].  K is at most 256; a and b have the same format, K and P."""
     dev, K = a._dev, a._K
     T = _offsets(offsets, dev)
     if b is not None and b._dev != dev:
         raise ValueError("a and b must be on one device")
-    out = offsets.new_empty((T, K, K), dtype=_F32)
-    need = lib.adpsgd_mx_product_workspace(K, a._P, T)
-    work = offsets.new_empty(need + 7 >> 3)
+    out, work, need = _buffers or product_buffers(a, T, offsets)
     _run(lib.adpsgd_mx_product, dev, a._ref, None if b is None else b._ref, T, offsets.data_ptr(), out.data_ptr(),
          work.data_ptr(), need)
     return out

@@ -222,6 +222,31 @@ def test_mx_begin_refuses(A):
         eng.mx_begin(good, torch.zeros(K, P))
 
 
+@pytest.mark.parametrize("fails", ["adpsgd_mx_quantize", "adpsgd_mx_product_workspace", "adpsgd_mx_average_workspace"])
+def test_a_sync_that_fails_has_moved_nothing(A, monkeypatch, fails):
+    """Its buffers are there before anything is sent, and the counter restarts behind the last call."""
+    w = _const(K=3)
+    with A.Adpsgd.from_workload(w) as eng:
+        eng.local_steps(4)
+        eng.average_mx(products=True)
+        eng.local_steps(3)
+        before = [t.clone() for t in (eng.x, eng.mx_base, eng.mx_residual)]
+        real = getattr(A._native.lib, fails)
+        with monkeypatch.context() as m:
+            if fails.endswith("_workspace"):       # more than any GPU has: torch raises at once
+                m.setattr(A._native.lib, fails, lambda *a: 1 << 50)
+            else:
+                m.setattr(A._native.lib, fails, lambda *a: A.EINVAL)
+            with pytest.raises(RuntimeError):
+                eng.average_mx(A.MX_E4M3, products=True)
+        assert getattr(A._native.lib, fails) is real
+        assert eng.get_state().cnt == 3
+        for t, b in zip((eng.x, eng.mx_base, eng.mx_residual), before):
+            assert torch.equal(t, b)
+        base, res = before[1].cpu().numpy(), before[2].cpu().numpy()
+        _sync_is_of(A, eng, w, base, res, A.MX_E4M3)
+
+
 def test_engine_sync_of_a_larger_model(A):
     """Several chunks a tensor, tensors that share chunks, rows of many blocks."""
     import workloads as W
