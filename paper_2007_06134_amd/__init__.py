@@ -152,7 +152,7 @@ class Adpsgd:
                                       "sync, or with the model after the last one")
         with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
             if self.mx_base is None:
-                self.mx_base = torch.zeros((self.P,), device=self.device)
+                self.mx_base = torch.zeros((self.P,), device=self.device, dtype=torch.float32)
             if error_feedback and self.mx_residual is None:
                 self.mx_residual = torch.zeros_like(self._x_rows)[:, :self.P]
             if self._mx_rows is None or self._mx_rows.format != format:

@@ -247,6 +247,19 @@ def test_a_sync_that_fails_has_moved_nothing(A, monkeypatch, fails):
         _sync_is_of(A, eng, w, base, res, A.MX_E4M3)
 
 
+def test_torchs_default_type_does_not_matter(A):
+    w = _const(K=2)
+    old = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float64)
+    try:
+        with A.Adpsgd.from_workload(w) as eng:
+            eng.local_steps(2)
+            assert np.all(np.isfinite(eng.average_mx(products=True)[0]))
+            assert eng.mx_base.dtype == eng.mx_residual.dtype == torch.float32
+    finally:
+        torch.set_default_dtype(old)
+
+
 def test_engine_sync_of_a_larger_model(A):
     """Several chunks a tensor, tensors that share chunks, rows of many blocks."""
     import workloads as W
