@@ -406,8 +406,9 @@ ADPSGD_API int adpsgd_mx_quantize(const adpsgd_mx_rows *out, const float *x, int
                                   const float *residual_in, float *residual_out, int64_t residual_stride,
                                   void *stream);
 
-/* y [K][P] (rows y_stride elements apart, 0: P) = base + what was sent; base
- * [P] may be NULL and does not overlap y. */
+/* y [K][P] (rows y_stride elements apart, 0: P) = base + what was sent, rounded
+ * once (also where rows from elsewhere say numbers of 2^128 and more); base [P]
+ * may be NULL and does not overlap y. */
 ADPSGD_API int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *base, float *y, int64_t y_stride,
                                     void *stream);
 
@@ -415,7 +416,7 @@ ADPSGD_API int adpsgd_mx_dequantize(const adpsgd_mx_rows *rows, const float *bas
  * rows (one rounding to fp32), also written to every row of x [K][P] (rows
  * x_stride apart, 0: P), and var[tau] (device, [T]) = (1/K) sum_k sum_{i in
  * tau} (mean_i - row_k,i)^2 in 64 bits, as adpsgd_average's of the replicas base
- * + row.  base, base_out and x may be NULL; base_out may be base; else no two of
+ * + row.  Numbers of 2^128 and more count as what they are.  base, base_out and x may be NULL; base_out may be base; else no two of
  * them overlap.
  * tensor_offsets[T+1] is in device memory, as for adpsgd_init (T in [1, 2^24]);
  * its values are not read back: others than offsets[0] = 0 <= ... <=
@@ -433,7 +434,8 @@ ADPSGD_API int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
  * (b NULL or a itself: of one set with itself, a symmetric matrix; then
  * (tr C - 1'C1 / K) / K is adpsgd_mx_average's variance).  Sums of up to 16384
  * products are taken in fp32 (E4M3: in two levels), the rest in 64 bits.  E4M3
- * elements below 2^-126 are rounded to multiples of 2^-133.  tensor_offsets and
+ * elements below 2^-126 are rounded to multiples of 2^-133, and those of 2^128 and
+ * more (quantize sends none) count as infinite.  tensor_offsets and
  * workspace (adpsgd_mx_product_workspace bytes) as above.  Both workspace
  * functions return 0 for invalid arguments. */
 ADPSGD_API size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T);

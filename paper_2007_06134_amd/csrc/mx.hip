@@ -101,6 +101,23 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
     return __uint_as_float(b > 0x400000u ? b : 0x400000u);
 }
 
+// The same numbers in 64 bits, where none is too large (those of rows from elsewhere may
+// be 2^128 and more, which decode makes infinite: from scale byte kFarByte on).
+template <int F>
+constexpr uint32_t kFarByte = 254 - Fmt<F>::kTopExp + 1;
+struct Wide {
+    double v[4];
+};
+template <int F>
+__device__ __forceinline__ Wide decode_wide(uint32_t c, uint32_t byte) {
+    const f4 v = Fmt<F>::decode(c, 1.f);
+    const uint64_t s = byte == 255 ? 0x7ff8ull << 48 : (uint64_t)(byte + 1023 - 127) << 52;
+    Wide w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w.v[j] = (double)v[j] * __builtin_bit_cast(double, s);
+    return w;
+}
+
 // The largest of the 8 lanes that hold a block (unsigned compare: of magnitudes'
 // bits, so that a NaN is the largest).
 __device__ __forceinline__ uint32_t max_of_8_lanes(uint32_t v) {
@@ -344,7 +361,14 @@ __device__ __forceinline__ void dequantize_chunk(const DequantizeParams &p, int3
     for (int i = 0; i < R; ++i) {
         if (k0 + i >= p.K) break;
         f4 v = Fmt<F>::decode(c[i], scale_of(s[i]));
-        if (p.base) v = b + v;
+        if (p.base) {
+            v = b + v;
+            if (s[i] >= kFarByte<F>) {      // (a sum that 64 bits do not hold is no tie in 24: rounded as once)
+                const Wide w = decode_wide<F>(c[i], s[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = (float)((double)b[j] + w.v[j]);
+            }
+        }
         store4<NT, Full>(p.y + (k0 + i) * p.y_ld, e, p.P, v);
     }
 }
@@ -443,6 +467,33 @@ __device__ __forceinline__ void average_chunk(const AverageParams &p, int64_t c0
         }
     }
     *bound = boundary_from(edge, c0);
+    // Numbers of 2^128 and more are infinite as fp32, their sums need not be: where one is not
+    // finite the wave reads its rows again, in 64 bits.  (Ordinary rows pay one addition an element;
+    // K = 8, P = 138M 1085 us, 1086 without.)
+    double most = 0.0;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most += s2[u][j];
+    if (__any(!(most < __builtin_inf()))) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            int64_t place = c0 + u * (kThreads * 4) + threadIdx.x * 4;
+            if (!Full && place >= p.P) place = (p.P - 1) / 4 * 4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s1[u][j] = s2[u][j] = 0.0;
+#pragma unroll 1
+            for (int32_t k = 0; k < p.K; ++k) {
+                const Wide w = decode_wide<F>(*reinterpret_cast<const Code *>(p.codes + k * p.code_ld + (place >> 2) * sizeof(Code)),
+                                              p.scales[k * p.scale_ld + (place >> 5)]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s1[u][j] += w.v[j];
+                    s2[u][j] = fma(w.v[j], w.v[j], s2[u][j]);
+                }
+            }
+        }
+    }
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         const int64_t e = e0 + u * (kThreads * 4);

@@ -1,0 +1,111 @@
+"""What the microscaled calls do at the edges of their arguments: rows whose numbers pass fp32."""
+import numpy as np
+import pytest
+import torch
+
+import mx_reference as ref
+from test_gpu_mx import _rows, _same
+
+pytestmark = pytest.mark.gpu
+
+FORMATS = [ref.E2M1, ref.E4M3]
+
+
+@pytest.fixture(scope="module")
+def A():
+    assert torch.cuda.is_available()
+    import paper_2007_06134_amd as A
+    return A
+
+
+def _far_rows(rng, K, P, fmt):
+    """Codes and scale bytes as a sender of another make may have them: all codes but NaN, scales up to
+    2^127, so that many numbers pass fp32; ordinary and NaN blocks among them."""
+    n = -(-P // 32)
+    codes = rng.integers(0, 256, (K, n * (16 if fmt == ref.E2M1 else 32)), dtype=np.uint8)
+    if fmt == ref.E4M3:
+        codes[codes % 128 == 127] = 0x7E
+    byte = rng.integers(240, 255, (K, n)).astype(np.uint8)
+    byte[:, rng.random(n) < 0.3] = 127
+    byte[K - 1, n // 2] = 255
+    return codes, byte
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("K,P", [(2, 33), (4, 3001), (9, 70_001), (17, 2000), (2, 4_300_001)])
+def test_average_of_numbers_past_fp32(A, fmt, K, P):
+    """Their sums are 64-bit ones, so opposite numbers of 2^128 and more cancel; what does not fit is an
+    infinity in the model only."""
+    rng = np.random.default_rng([fmt, K, P, 5])
+    codes, byte = _far_rows(rng, K, P, fmt)
+    if K % 2 == 0:       # half of the workers send the other half's negatives, but for one element
+        h = K // 2
+        codes[h:] = codes[:h] ^ (0x88 if fmt == ref.E2M1 else 0x80)
+        byte[h:] = byte[:h]
+        byte[K - 1, 0] = 127
+    v = ref.values(codes, byte, P, fmt)
+    off = np.array([0, 3, 3, 32, P])
+    base = rng.standard_normal(P).astype(np.float32)
+    rows, offd = _rows(A, codes, byte, P, fmt), torch.from_numpy(off).cuda()
+    for b in (None, base):
+        new, want = ref.average(v, off, b)
+        x = torch.empty((K, P), device="cuda")
+        got, var = A.mx_average(rows, offd, None if b is None else torch.from_numpy(b).cuda(), x=x)
+        got, var = got.cpu().numpy().astype(np.float64), var.cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(new)) and np.array_equal(np.isnan(var), np.isnan(want))
+        ok = ~np.isnan(new)
+        most = np.float64(np.finfo(np.float32).max)
+        fits = ok & (np.abs(new) <= most)
+        past = ok & (np.abs(new) >= 2.0 ** 128 * (1 - 2.0 ** -25))
+        # (a mean of K numbers that are not powers of two apart is rounded in 64 bits first)
+        assert np.all(np.abs(got - new)[fits] <= 2.0 ** -24 * (1 + 1e-6) * np.abs(new)[fits] + 2.0 ** -149)
+        assert np.all(np.isinf(got[past])) and np.all(np.signbit(got[past]) == np.signbit(new[past]))
+        ok = ~np.isnan(want)
+        assert ok.any() and np.all(np.abs(var - want)[ok] <= 1e-12 * want[ok])
+        assert _same(x.cpu().numpy(), np.repeat(got[None].astype(np.float32), K, 0))
+    if K % 2 == 0:
+        assert np.all(new[~np.isnan(new)][40:] == base[~np.isnan(new)][40:])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("K", [1, 3, 7])
+def test_read_back_of_numbers_past_fp32(A, fmt, K):
+    """base + number, rounded once: finite where the sum is."""
+    P = 5000
+    rng = np.random.default_rng([fmt, K, 6])
+    codes, byte = _far_rows(rng, K, P, fmt)
+    v = ref.values(codes, byte, P, fmt)
+    base = (rng.uniform(-1, 1, P) * 2.0 ** 128 * (1 - 2.0 ** -24)).astype(np.float32)
+    rows = _rows(A, codes, byte, P, fmt)
+    with np.errstate(over="ignore"):
+        assert _same(A.mx_dequantize(rows).cpu().numpy(), v.astype(np.float32))
+        want = base.astype(np.float64) + v
+        rescued = (np.abs(v) >= 2.0 ** 128) & (np.abs(want) < 2.0 ** 127)
+        assert rescued.sum() > 10
+        assert _same(A.mx_dequantize(rows, torch.from_numpy(base).cuda()).cpu().numpy(), want.astype(np.float32))
+
+
+def test_four_bit_products_of_numbers_past_fp32(A):
+    """The matrix instruction applies both scales to the product: 6 * 2^127 against numbers near 2^-127."""
+    P = 64
+    rng = np.random.default_rng(3)
+    codes = rng.integers(0, 256, (2, 4, P // 2), dtype=np.uint8)
+    byte = np.stack([np.full((4, 2), 254, np.uint8), np.array([[0, 0], [1, 1], [2, 0], [120, 121]], np.uint8)])
+    v, w = (ref.values(codes[i], byte[i], P, ref.E2M1) for i in range(2))
+    got = A.mx_product(_rows(A, codes[0], byte[0], P, ref.E2M1), torch.tensor([0, P], device="cuda"),
+                       _rows(A, codes[1], byte[1], P, ref.E2M1)).cpu().numpy()[0]
+    assert np.array_equal(got.astype(np.float64), v @ w.T)       # (quarters of integers up to 144, under few scales)
+
+
+def test_eight_bit_products_of_numbers_past_fp32(A):
+    """The operands are bf16 numbers: those of 2^128 and more count as infinite, so their products do."""
+    P = 32
+    codes = np.full((2, 1, P), 0x38, np.uint8)        # 1
+    codes[0, 0, 3] = 0x7E                             # 448
+    byte = np.array([[[246]], [[127]]], np.uint8)     # 448 * 2^119 < 2^128
+    offs = torch.tensor([0, P], device="cuda")
+    other = _rows(A, codes[1], byte[1], P, ref.E4M3)
+    got = A.mx_product(_rows(A, codes[0], byte[0], P, ref.E4M3), offs, other).item()
+    assert got == 479 * 2.0 ** 119
+    got = A.mx_product(_rows(A, codes[0], byte[0] + 8, P, ref.E4M3), offs, other).item()
+    assert got == np.inf
