@@ -56,6 +56,9 @@ class MxRows:
         dev = codes.get_device()
         if K != K2 or scales.get_device() != dev:
             raise ValueError("codes and scales must have one row a worker on one device")
+        if not 1 <= K <= 65536:
+            raise ValueError("there must be 1 to 65536 rows")
+        _check_size(K, P)
         self._codes, self._scales, self._P, self._format, self._K, self._dev = codes, scales, P, format, K, dev
         self._c = adpsgd_mx_rows(codes.data_ptr(), scales.data_ptr(), code_ld, scale_ld, P, K, format)
         self._ref = C.byref(self._c)
@@ -65,10 +68,9 @@ class MxRows:
         """Rows to be written, at adpsgd_mx_code_stride and adpsgd_mx_scale_stride."""
         if format not in _ROW_BYTES:
             raise ValueError("format must be MX_E2M1 or MX_E4M3")
-        if K < 1 or P < 0:
-            raise ValueError("K must be >= 1 and P >= 0")
-        if P > 1 << 34:
-            raise ValueError("P must be at most 2^34")
+        if not 1 <= K <= 65536 or P < 0:
+            raise ValueError("K must be in [1, 65536] and P >= 0")
+        _check_size(K, P)
         return cls(torch.empty((K, lib.adpsgd_mx_code_stride(format, P)), dtype=_U8, device=device),
                    torch.empty((K, lib.adpsgd_mx_scale_stride(P)), dtype=_U8, device=device), P, format)
 
@@ -78,6 +80,12 @@ class MxRows:
     P = property(lambda self: self._P)
     format = property(lambda self: self._format)
     device = property(lambda self: self._codes.device)
+
+
+def _check_size(K: int, P: int) -> None:
+    """The library's limits, before memory of that size is asked for."""
+    if P > 1 << 34 or (P + 255 >> 8) * K >= 1 << 31:
+        raise ValueError("P must be at most 2^34 and K * P below 2^39")
 
 
 def _bytes(t: torch.Tensor, need: int, name: str) -> Tuple[int, int]:
@@ -211,6 +219,9 @@ def mx_product(a: MxRows, offsets: torch.Tensor, b: Optional[MxRows] = None, *,
     T = _offsets(offsets, dev)
     if b is not None and b._dev != dev:
         raise ValueError("a and b must be on one device")
+    if K > 256 or (b is not None and (b._format != a._format or b._K != K or b._P != a._P)):
+        # (the library says why, before any memory is taken)
+        _run(lib.adpsgd_mx_product, dev, a._ref, None if b is None else b._ref, T, offsets.data_ptr(), None, None, 0)
     out, work, need = _buffers or product_buffers(a, T, offsets)
     _run(lib.adpsgd_mx_product, dev, a._ref, None if b is None else b._ref, T, offsets.data_ptr(), out.data_ptr(),
          work.data_ptr(), need)

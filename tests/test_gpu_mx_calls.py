@@ -1,4 +1,5 @@
-"""What the microscaled calls do at the edges of their arguments: rows whose numbers pass fp32."""
+"""What the microscaled calls do at the edges of their arguments: rows whose numbers pass fp32, and
+what is refused before memory is taken for it."""
 import numpy as np
 import pytest
 import torch
@@ -109,3 +110,31 @@ def test_eight_bit_products_of_numbers_past_fp32(A):
     assert got == 479 * 2.0 ** 119
     got = A.mx_product(_rows(A, codes[0], byte[0] + 8, P, ref.E4M3), offs, other).item()
     assert got == np.inf
+
+
+def _allocations():
+    return torch.cuda.memory_stats()["allocation.all.allocated"]
+
+
+def test_what_the_library_refuses_takes_no_memory(A):
+    """Thousands of workers' products, or more rows than a call takes: the refusal, not a failed
+    allocation of what the call would have written."""
+    off = torch.tensor([0, 10], device="cuda")
+    many = A.MxRows(torch.zeros((3000, 16), dtype=torch.uint8, device="cuda"),
+                    torch.zeros((3000, 16), dtype=torch.uint8, device="cuda"), 10)
+    n = _allocations()
+    with pytest.raises(A.AdpsgdError, match="256") as e:
+        A.mx_product(many, off)
+    assert e.value.code == A.EINVAL and _allocations() == n
+    one = A.mx_quantize(torch.zeros((4, 10), device="cuda"))
+    two = A.mx_quantize(torch.zeros((4, 10), device="cuda"), format=A.MX_E4M3)
+    n = _allocations()
+    with pytest.raises(A.AdpsgdError, match="same format"):
+        A.mx_product(one, off, two)
+    assert _allocations() == n
+    x, b = torch.zeros((65537, 1), device="cuda"), torch.zeros((65537, 16), dtype=torch.uint8, device="cuda")
+    n = _allocations()
+    for call in (lambda: A.mx_quantize(x), lambda: A.MxRows(b, b, 1)):
+        with pytest.raises(ValueError, match="65536"):
+            call()
+    assert _allocations() == n
