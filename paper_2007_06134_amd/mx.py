@@ -6,6 +6,11 @@ elements sharing a power of two.  Every function runs on the current stream of
 its tensors' device, waits for nothing and can be captured into a graph;
 outputs and workspaces that the caller does not pass come from torch's
 allocator.
+
+No gradient flows through a call: tensors that require one are refused unless
+gradients are switched off (``torch.no_grad()``).  What a call writes then counts
+for autograd as torch's own writes do; writes to tensors that require no
+gradient are not counted, as those of the engine are not.
 """
 from __future__ import annotations
 
@@ -22,6 +27,7 @@ _ROW_BYTES = {MX_E2M1: 16, MX_E4M3: 32}   # of codes, a block
 # The smallest calls take a few microseconds on the GPU, so the checks below are
 # made of the cheapest queries of a tensor (a device is its index, -1 off the GPU).
 _U8, _F32, _F64, _I64 = torch.uint8, torch.float32, torch.float64, torch.int64
+_gradients = torch.is_grad_enabled
 _current_device = torch._C._cuda_getDevice
 _current_stream = torch._C._cuda_getCurrentRawStream
 
@@ -99,10 +105,17 @@ def _bytes(t: torch.Tensor, need: int, name: str) -> Tuple[int, int]:
     return K, t.stride(0) if K > 1 and w > 0 else -(-w // 16) * 16
 
 
+def _no_grad(name: str) -> None:
+    if _gradients():
+        raise ValueError(f"{name} requires a gradient, and none flows through this call: use torch.no_grad() or detach()")
+
+
 def _matrix(t: torch.Tensor, K: int, P: int, dev: int, name: str) -> int:
     """Row stride of a float32 [K, P] tensor."""
     if t.dtype is not _F32 or t.shape != (K, P) or t.get_device() != dev:
         raise ValueError(f"{name} must be float32 [{K}, {P}] on device {dev}")
+    if t.requires_grad:
+        _no_grad(name)
     return _row_stride(t, K, P, name)
 
 
@@ -122,7 +135,16 @@ def _vector(t: Optional[torch.Tensor], P: int, dev: int, name: str) -> Optional[
         return None
     if t.dtype is not _F32 or t.dim() != 1 or t.numel() != P or t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous float32 [{P}] on device {dev}")
+    if t.requires_grad:
+        _no_grad(name)
     return t.data_ptr()
+
+
+def _written(*tensors: Optional[torch.Tensor]) -> None:
+    """Of a call without gradients (with them it takes no tensor that this is for)."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            torch.autograd.graph.increment_version(t)
 
 
 def _offsets(t: torch.Tensor, dev: int) -> int:
@@ -142,6 +164,8 @@ def mx_quantize(x: torch.Tensor, base: Optional[torch.Tensor] = None, residual: 
     dev = x.get_device()
     if x.dtype is not _F32 or x.dim() != 2 or dev < 0:
         raise ValueError("x must be a float32 matrix on a GPU")
+    if x.requires_grad:
+        _no_grad("x")
     K, P = x.shape
     x_ld = _row_stride(x, K, P, "x")
     base_ptr = _vector(base, P, dev, "base")
@@ -161,6 +185,8 @@ def mx_quantize(x: torch.Tensor, base: Optional[torch.Tensor] = None, residual: 
     elif out._K != K or out._P != P or out._dev != dev or (format is not None and format != out._format):
         raise ValueError(f"out must be rows of the format for [{K}, {P}] on device {dev}")
     _run(lib.adpsgd_mx_quantize, dev, out._ref, x.data_ptr(), x_ld, base_ptr, r_in, r_out, r_ld)
+    if not _gradients():
+        _written(residual if residual_out is None else residual_out)
     return out
 
 
@@ -173,6 +199,8 @@ def mx_dequantize(rows: MxRows, base: Optional[torch.Tensor] = None, *,
         out = torch.empty((rows._K, rows._P), dtype=_F32, device=rows._codes.device)
     ld = _matrix(out, rows._K, rows._P, dev, "out")
     _run(lib.adpsgd_mx_dequantize, dev, rows._ref, base_ptr, out.data_ptr(), ld)
+    if not _gradients():
+        _written(out)
     return out
 
 
@@ -208,6 +236,8 @@ def mx_average(rows: MxRows, offsets: torch.Tensor, base: Optional[torch.Tensor]
     var, work, need = _buffers or average_buffers(rows, T, offsets)
     _run(lib.adpsgd_mx_average, dev, rows._ref, T, offsets.data_ptr(), base_ptr, out_ptr, x_ptr, x_ld, var.data_ptr(),
          work.data_ptr(), need)
+    if not _gradients():
+        _written(x, base_out)
     return base_out, var
 
 

@@ -1,5 +1,5 @@
-"""What the microscaled calls do at the edges of their arguments: rows whose numbers pass fp32, and
-what is refused before memory is taken for it."""
+"""What the microscaled calls do at the edges of their arguments: rows whose numbers pass fp32,
+what is refused before memory is taken for it, tensors that take part in autograd."""
 import numpy as np
 import pytest
 import torch
@@ -138,3 +138,48 @@ def test_what_the_library_refuses_takes_no_memory(A):
         with pytest.raises(ValueError, match="65536"):
             call()
     assert _allocations() == n
+
+
+def _calls(A, K=3, P=100):
+    """(name, call with that tensor, the tensor) of every float tensor that a call takes."""
+    z = lambda *s: torch.zeros(s, device="cuda")      # noqa: E731
+    off = torch.tensor([0, P], device="cuda")
+    rows = A.mx_quantize(z(K, P))
+    return [("x", lambda t: A.mx_quantize(t), z(K, P)), ("base", lambda t: A.mx_quantize(z(K, P), t), z(P)),
+            ("residual", lambda t: A.mx_quantize(z(K, P), None, t), z(K, P)),
+            ("residual_out", lambda t: A.mx_quantize(z(K, P), residual_out=t), z(K, P)),
+            ("base", lambda t: A.mx_dequantize(rows, t), z(P)), ("out", lambda t: A.mx_dequantize(rows, out=t), z(K, P)),
+            ("base", lambda t: A.mx_average(rows, off, t), z(P)), ("x", lambda t: A.mx_average(rows, off, x=t), z(K, P)),
+            ("base_out", lambda t: A.mx_average(rows, off, base_out=t), z(P))]
+
+
+def test_tensors_that_record_gradients_are_refused(A):
+    """No gradient flows through the calls: silently cutting the graph is an error, under no_grad it is asked for."""
+    for name, call, t in _calls(A):
+        t.requires_grad_()
+        with pytest.raises(ValueError, match=name + ".*no_grad"):
+            call(t)
+        with torch.no_grad():
+            call(t)
+
+
+def test_writes_under_no_grad_are_seen_by_autograd(A):
+    """A parameter that an earlier graph saved and a call then writes: its backward raises, as after torch's own
+    writes, in place of taking the new values."""
+    for name, call, t in _calls(A):
+        t.requires_grad_()
+        y = (t * t).sum()
+        with torch.no_grad():
+            call(t)
+        # (residual is written where there is no residual_out)
+        if name in ("residual", "residual_out", "out", "base_out") or (name == "x" and t._version):
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                y.backward()
+        else:
+            y.backward()
+    t = torch.zeros((3, 100), device="cuda", requires_grad=True)
+    rows, off = A.mx_quantize(torch.ones((3, 100), device="cuda")), torch.tensor([0, 100], device="cuda")
+    before = t._version
+    with torch.no_grad():
+        A.mx_average(rows, off, x=t)
+    assert t._version > before
