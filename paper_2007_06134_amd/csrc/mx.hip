@@ -713,6 +713,15 @@ __device__ __forceinline__ void multiply(const u4 *a, const uint32_t *sa, const 
     }
 }
 
+// Between what a wave's lanes write to LDS and what its other lanes read there, both ways.  The
+// hardware takes a wave's LDS operations in order, so it needs no instruction (as many with it as
+// without); it is the compiler that may not move one past another.
+__device__ __forceinline__ void lds_turn() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // 256 bytes of codes, kElems elements, of each row of a wave's tiles in LDS.
 template <int TILES>
 struct WaveLds {
@@ -911,14 +920,14 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
         if (kPacked && stretches > 1) {      // the stretches' parts of the tile, summed
             float *at = parts + wave * 256;
             park(at);
-            __builtin_amdgcn_wave_barrier();
+            lds_turn();
             for (int e = l; e < p.R * p.R; e += 64) {
                 const int32_t row = e >> p.log_r, col = e & (p.R - 1);
                 double s = 0.0;
                 for (int g = 0; g < stretches; ++g) s += at[(g * p.R + row) * 16 + g * p.R + col];
                 put(out, mirror, row, col, (float)s);
             }
-            __builtin_amdgcn_wave_barrier();
+            lds_turn();
             return;
         }
         // (32-bit indexes from a scalar base; most matrices fill their tiles)
@@ -956,8 +965,10 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     if (__builtin_amdgcn_readlane(bound, tau - from) <= 0 && __builtin_amdgcn_readlane(bound, tau - from + 1) >= b1 - b0 &&
         b1 <= p.P) {
         while (s0 < c1) {
+            lds_turn();
             a.stash(mine, 0);
             if (!kOne) o.stash(mine, NT);
+            lds_turn();
             s0 += super;
             if (s0 < c1) {      // (on their way while these are multiplied)
                 a.template load<true>(s0 / kElems + fetched, p.P);
@@ -967,6 +978,7 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
             level();
         }
         join();
+        lds_turn();
         float *at = kPacked ? parts : reinterpret_cast<float *>(shared);
         constexpr int kStride = kPacked ? 256 : sizeof(WaveLds<TILES>) / sizeof(float);   // of waves
         park(at + wave * kStride);
@@ -1005,8 +1017,10 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     bool open = false;             // acc holds something of tensor tau
     for (int32_t at = 0; at < size;) {
         const int32_t next = at + span < size ? at + span : size;
+        lds_turn();
         a.stash(mine, 0);
         if (!kOne) o.stash(mine, NT);
+        lds_turn();
         if (next < size) {
             a.template load<false>((c0 + next) / kElems + fetched, p.P);
             if (!kOne) o.template load<false>((c0 + next) / kElems + fetched, p.P);
