@@ -433,7 +433,8 @@ ADPSGD_API int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
  * b_k,i of the rows of two sets of messages of the same format, K <= 256 and P
  * (b NULL or a itself: of one set with itself, a symmetric matrix; then
  * (tr C - 1'C1 / K) / K is adpsgd_mx_average's variance).  Sums of up to 16384
- * products are taken in fp32 (E4M3: in two levels), the rest in 64 bits.  E4M3
+ * products are taken in fp32, in two levels (some 512 products, then those sums),
+ * and joined in 64 bits, rounded to fp32 once on the way and at the end.  E4M3
  * elements below 2^-126 are rounded to multiples of 2^-133, and those of 2^128 and
  * more (quantize sends none) count as infinite.  tensor_offsets and
  * workspace (adpsgd_mx_product_workspace bytes) as above.  Both workspace

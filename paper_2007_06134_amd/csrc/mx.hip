@@ -873,11 +873,15 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
     };
-    // E4M3: two levels of fp32 sums, acc over 256 bytes of each row and total of those.  (Error
-    // against 64 bits at K = 16, P = 25.6M 3.1e-8 of the result; 5.5e-7 with one level.  K = 16 82 us
-    // either way, K = 32, P = 20M 128 and 125.  Sums of 4-bit products are mostly exact: 2.6e-8.)
-    constexpr bool kLevels = F == ADPSGD_MX_E4M3;
-    v4 total[kLevels ? NT : 1][kLevels ? NT : 1];
+    // Two levels of fp32 sums: acc over 256 bytes of each row and total of those.  (Error against 64 bits in 8 bits at
+    // K = 16, P = 25.6M 3.1e-8 of the result, 5.5e-7 with one level; in 4 bits, whose sums are exact only where
+    // scales are alike, 3.0e-7 and 5.2e-7 of 48 workers' blocks of many sizes, 1.1e-7 and 3.8e-6 of small products
+    // beside a large one, K = 70.  4 bits, us, and with one level: K = 8, P = 138M 106 and 106, K = 32, P = 20M 72 and 72,
+    // K = 33, P = 20M 83 and 79, K = 64, P = 5M 42 and 42, K = 256, P = 4.3M 405 and 400.)
+    // A piece of less than that before or behind a tensor's whole ones is a level by itself,
+    // but of three or four tiles of 4 bits joins its neighbour's (K = 100, P = 5M in 10 tensors 132 us, 139 by itself).
+    constexpr bool kPieces = F == ADPSGD_MX_E4M3 || NT <= 2;
+    v4 total[NT][NT];
     auto each = [&](auto f) {
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -885,18 +889,19 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
             for (int j = kOne ? i : 0; j < NT; ++j) f(i, j);
     };
     auto level = [&] {
-        if constexpr (kLevels) each([&](int i, int j) {
+        each([&](int i, int j) {
             total[i][j] += acc[i][j];
             acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
         });
     };
     auto join = [&] {
-        if constexpr (kLevels) each([&](int i, int j) {
-            acc[i][j] = total[i][j];
+        each([&](int i, int j) {
+            if (kPieces) acc[i][j] = total[i][j];
+            else acc[i][j] += total[i][j];
             total[i][j] = v4{0.f, 0.f, 0.f, 0.f};
         });
     };
-    if constexpr (kLevels) each([&](int i, int j) { total[i][j] = v4{0.f, 0.f, 0.f, 0.f}; });
+    each([&](int i, int j) { total[i][j] = v4{0.f, 0.f, 0.f, 0.f}; });
     auto park = [&](float *at) {
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -1043,13 +1048,13 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
                 open = true;
                 if (hi - lo == span) {
                     multiply_super<F, NT, kOne, false>(mine, masks, 0, kElems, 0, 16, acc);
-            level();
+                    level();
                 } else {
                     // what of this lane's row is the tensor's
                     const int first = at + held * kElems, f = lo - first, t = hi - first;
                     const int unit0 = (lo - at) / Masks<F>::kUnit, units = (hi - at - 1) / Masks<F>::kUnit - unit0 + 1;
                     multiply_super<F, NT, kOne, true>(mine, masks, f < 0 ? 0 : f, t > kElems ? kElems : t, unit0, units, acc);
-                        level();
+                    if (kPieces) level();
                 }
             }
             if (end > next) break;

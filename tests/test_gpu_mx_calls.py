@@ -1,5 +1,5 @@
 """What the microscaled calls do at the edges of their arguments: rows whose numbers pass fp32,
-what is refused before memory is taken for it, tensors that take part in autograd."""
+what is refused before memory is taken for it, tensors that take part in autograd, sums of products of many sizes."""
 import numpy as np
 import pytest
 import torch
@@ -183,3 +183,40 @@ def test_writes_under_no_grad_are_seen_by_autograd(A):
     with torch.no_grad():
         A.mx_average(rows, off, x=t)
     assert t._version > before
+
+
+# of a result whose products are all positive: a level of 512 elements is 4 matrix instructions of at most four
+# roundings, then at most 32 of those sums, the partial sum's rounding and the result's
+_LEVELS = (4 * 4 + 32 + 2) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("K", [1, 2, 4, 8, 16, 32, 48, 64, 70])
+def test_four_bit_products_of_blocks_of_many_sizes(A, K):
+    """Blocks whose sizes differ by a decade or so: sums of few products are no longer exact."""
+    P = 600_000
+    g = torch.Generator(device="cuda").manual_seed(K)
+    size = torch.exp(2.3 * torch.randn((K, P // 32), device="cuda", generator=g)).repeat_interleave(32, 1)
+    x = size * (torch.rand((K, P), device="cuda", generator=g) + 0.1)
+    rows = A.mx_quantize(x)
+    v = A.mx_dequantize(rows).double()
+    got = A.mx_product(rows, torch.tensor([0, P], device="cuda"))[0].double()
+    want = v @ v.t().contiguous()
+    off_by = ((got - want).abs() / want).max().item()
+    print(f"K={K}: {off_by:.2e} of the result")
+    assert off_by <= _LEVELS
+
+
+@pytest.mark.parametrize("K,P", [(8, 168_000_000), (16, 84_000_000), (32, 34_000_000), (64, 17_000_000), (70, 8_400_000)])
+def test_four_bit_products_keep_small_terms_beside_a_large_one(A, K, P):
+    """Every 16384 elements a 1, the rest 2^-16: 128 of their products are less than half a step of a sum that
+    holds the 1, 512 of them are a step of it.  One sum of 16384 products would lose 16352 * 2^-32, 3.8e-6."""
+    P -= P % 16384
+    codes = torch.full((K, P // 2), 0x22, dtype=torch.uint8, device="cuda")       # ones
+    scales = torch.full((K, P // 32), 127 - 16, dtype=torch.uint8, device="cuda")
+    scales[:, ::512] = 127
+    codes.view(K, -1, 16)[:, ::512] = 0
+    codes.view(K, -1, 16)[:, ::512, 0] = 0x02
+    got = A.mx_product(A.MxRows(codes, scales, P), torch.tensor([0, P], device="cuda"))[0].double().cpu()
+    want = (P // 16384) * (1 + 16352 * 2.0 ** -32)
+    print(f"K={K}: {((got - want).abs().max() / want).item():.2e} of the result")
+    assert bool(((got - want).abs() <= _LEVELS * want).all())
