@@ -879,7 +879,7 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     // beside a large one, K = 70.  4 bits, us, and with one level: K = 8, P = 138M 106 and 106, K = 32, P = 20M 72 and 72,
     // K = 33, P = 20M 83 and 79, K = 64, P = 5M 42 and 42, K = 256, P = 4.3M 405 and 400.)
     // A piece of less than that before or behind a tensor's whole ones is a level by itself,
-    // but of three or four tiles of 4 bits joins its neighbour's (K = 100, P = 5M in 10 tensors 132 us, 139 by itself).
+    // but of three or four tiles of 4 bits joins its neighbour's (K = 100, P = 5M in 10 tensors 131 us, 139 by itself).
     constexpr bool kPieces = F == ADPSGD_MX_E4M3 || NT <= 2;
     v4 total[NT][NT];
     auto each = [&](auto f) {
