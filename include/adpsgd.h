@@ -437,8 +437,8 @@ ADPSGD_API int adpsgd_mx_average(const adpsgd_mx_rows *rows, int32_t T, const in
  * and joined in 64 bits, rounded to fp32 once on the way and at the end.  E4M3
  * elements below 2^-126 are rounded to multiples of 2^-133, and those of 2^128 and
  * more (quantize sends none) count as infinite.  tensor_offsets and
- * workspace (adpsgd_mx_product_workspace bytes) as above.  Both workspace
- * functions return 0 for invalid arguments. */
+ * workspace (adpsgd_mx_product_workspace bytes: up to 16 MB + P K^2 / 4096 + 4 T K^2)
+ * as above.  Both workspace functions return 0 for invalid arguments. */
 ADPSGD_API size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T);
 ADPSGD_API int adpsgd_mx_product(const adpsgd_mx_rows *a, const adpsgd_mx_rows *b, int32_t T,
                                  const int64_t *tensor_offsets, float *out, void *workspace, size_t workspace_bytes,

@@ -404,14 +404,15 @@ struct AverageParams {
     double inv_k;
 };
 
-// Sums in 64 bits: of numbers with at most four significant bits the sums over
-// the workers, s1 of d and s2 of d^2, are exact unless their scales are some 2^20
-// apart (where the smaller hardly count), so K s2 - s1^2 = K sum_k (d_k - mean)^2
-// loses nothing where the workers agree, and one pass over the rows is enough.
+// Sums in 64 bits, s1 of d and s2 of d^2 over the workers, so that one pass over the rows is enough:
+// numbers have at most four significant bits.  Either an element's are equal for all workers, and K s2 and s1^2
+// come out the same; or two of them differ by a sixteenth of the largest, and K s2 - s1^2 = K sum_k (d_k - mean)^2
+// is at least s2 / 512, of which the roundings of the sums (none where the blocks' scales are alike: 12 (E2M1) or
+// 2^18 (E4M3) steps at most, squared, in 53 bits) are K^2 2^-44 at most.
 // What bounds it is the writing of K rows: at K = 8, P = 138M 1.08 ms, 5.6 TB/s.
 // The codes of eight rows are loaded before any is used (a row at a time: 1.72 ms), of
-// sixteen where a lane has one group of each (K = 32, P = 1.2M, 8 bits: 47.8 us; 49.2
-// with eight, 49.2 with 32).
+// sixteen where a lane has one group of each (us, and with eight: K = 32, P = 1.2M, 8 bits 47.6 and 49.0, 4 bits
+// 41.8 and 43.1; K = 64, P = 65K 15.6 and 16.8; K = 100, P = 1M 89.7 and 91.1; 49.2 with 32 in the first).
 constexpr int kAverageGroups = 2;  // float4 groups of a lane in a large problem
 
 template <int F, int NU, bool NT, bool Full>
@@ -836,8 +837,8 @@ enum { kOneGroup = 0, kUpper = 1, kEvery = 2 };
 //
 // NT: tiles of 16 rows of an operand that a wave holds at once (of one group, those
 // below the diagonal are left out).  The pairs of groups of the same elements follow each
-// other on one XCD, whose L2 gives the rows to all but the first (K = 256, P = 4M 430 us,
-// 767 with the pairs apart; two sets of 128, P = 5M 230 and 359).
+// other on one XCD, whose L2 gives the rows to all but the first (K = 256, P = 4M, groups of 32, 430 us,
+// 767 with the pairs apart; two sets of 128, P = 5M 232 and 359).
 template <int F, int NT, int Pairs>
 __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     constexpr bool kOne = Pairs == kOneGroup;
@@ -876,8 +877,8 @@ __global__ void __launch_bounds__(kThreads) k_mx_product(ProductParams p) {
     // Two levels of fp32 sums: acc over 256 bytes of each row and total of those.  (Error against 64 bits in 8 bits at
     // K = 16, P = 25.6M 3.1e-8 of the result, 5.5e-7 with one level; in 4 bits, whose sums are exact only where
     // scales are alike, 3.0e-7 and 5.2e-7 of 48 workers' blocks of many sizes, 1.1e-7 and 3.8e-6 of small products
-    // beside a large one, K = 70.  4 bits, us, and with one level: K = 8, P = 138M 106 and 106, K = 32, P = 20M 72 and 72,
-    // K = 33, P = 20M 83 and 79, K = 64, P = 5M 42 and 42, K = 256, P = 4.3M 405 and 400.)
+    // beside a large one, K = 70.  4 bits, us, and with one level: K = 8, P = 138M 106 and 106, K = 32, P = 20M 72
+    // and 72, K = 33, P = 20M 83 and 79, K = 64, P = 5M 42 and 42, K = 256, P = 4.3M 405 and 400.)
     // A piece of less than that before or behind a tensor's whole ones is a level by itself,
     // but of three or four tiles of 4 bits joins its neighbour's (K = 100, P = 5M in 10 tensors 131 us, 139 by itself).
     constexpr bool kPieces = F == ADPSGD_MX_E4M3 || NT <= 2;
@@ -1274,14 +1275,16 @@ int32_t tile_workers(int32_t K, int64_t P) {
 
 // Elements of a product's wave: of as many waves as the compute units hold evenly, four to
 // a block and 256 blocks a step (us, with this many waves a unit).  20 of the kernels for
-// up to 16 workers (K = 8, P = 138M: 106; 108 with 32; K = 16, P = 25.6M, 8 bits: 87, 94
-// with 32, 92 with 16), 8 for up to 32 (K = 24, P = 5M: 24.8; 25.5 with 12, 28.3 with 13,
-// 26.4 with 4; K = 32, P = 20M: 73, 78 with 12, 85 with 13), 4 for up to 64 (K = 64, P =
-// 5M: 49; 58 with 2, 60 with 5, 57 with 8), and a whole number of fours where more are
-// needed (two sets of 40, P = 20M: 164 with 8, 209 with 5).  More workers fill the units
-// with pairs of groups: fewer waves, so that the K x K partial sums come to 8 MB at most.
+// up to 16 workers (K = 8, P = 138M: 105; 108 with 32; K = 16, P = 25.6M, 8 bits: 82, 88
+// with 32, 87 with 16), 8 for up to 32 (K = 24, P = 5M: 25; 28 with 12, 33 with 13; K = 32, P =
+// 20M: 72, 74 with 12, 83 with 13; many small tensors are better off with 8 than 4, K = 32, P = 1.2M in
+// 400 tensors 19.3 and 21.6, a single one with 4, K = 24, P = 5M 25 and 22.5), 4 for up to 64 (K = 64, P =
+// 5M: 42; 54 with 2, 55 with 5, 49 with 8), and a whole number of fours where more are
+// needed (two sets of 40, P = 20M: 169 with 8, 210 with 5).  More workers fill the units
+// with pairs of groups: fewer waves, so that the K x K partial sums come to 8 MB.
 // No wave takes less than its partial sums outweigh, nor more than 16384 elements of a
-// row (of which fp32 sums are taken).
+// row (of which fp32 sums are taken): rows longer than 16384 waves hold have P K^2 / 4096 bytes of
+// partial sums (K = 256, P = 2^22: 67 MB), of which blocks inside one tensor write and read a quarter.
 int64_t product_chunk(int32_t K, int64_t P) {
     const int64_t super = kSuper * (16 / tile_workers(K, P)), most = 32;
     const int64_t supers = (P + super - 1) / super, least = (15 * (int64_t)K + super - 1) / super;
@@ -1476,12 +1479,12 @@ extern "C" size_t adpsgd_mx_product_workspace(int32_t K, int64_t P, int32_t T) {
 namespace {
 
 // Groups of rows by K: the more a wave holds, the fewer times the rows are loaded, but
-// the fewer waves a compute unit holds.  us, E2M1, b is a: K = 64, P = 5M 67 as groups of
-// 32, 49 as one of 64; K = 33, P = 20M 140 as groups of 32, 84 as one of 64, 79 as one of
-// 48; K = 100 as groups of 32 and of 48 P = 5M 143 and 127, P = 0.5M 27 and 35; K = 256
-// P = 4.3M 435 and 379, P = 0.5M 69 and 75.  Two operands: K = 40, P = 5M 65 as groups of
-// 32, 52 as one of 48; K = 70 131 as nine pairs of 32, 118 as four of 48; K = 64 93 as
-// two groups of 32, 116 as two of 48.
+// the fewer waves a compute unit holds.  us, b is a, E2M1 (in brackets E4M3): K = 64, P = 5M 61 (105) as groups of
+// 32, 42 (69) as one of 64; K = 33, P = 20M 141 as groups of 32, 103 as one of 64, 83 as one of
+// 48; K = 100 as groups of 32 and of 48 P = 5M 142 and 128 (287 and 269), P = 0.5M 25 and 32; K = 256
+// P = 4.3M 478 and 405 (903 and 802), P = 0.5M 64 and 63.  Two operands: K = 40, P = 5M 64 as groups of
+// 32, 47 as one of 48; K = 70 130 as nine pairs of 32, 118 as four of 48; K = 64 88 (162) as
+// two groups of 32, 109 (195) as two of 48.
 template <int F, int NT, int Pairs>
 void launch_product(ProductParams &p, uint32_t pairs, hipStream_t st) {
     p.pairs = pairs;
