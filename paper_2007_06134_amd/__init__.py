@@ -6,6 +6,7 @@ torch supplies only device memory and the HIP stream.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Optional
 
 import numpy as np
@@ -126,6 +127,14 @@ class Adpsgd:
                 self.mx_begin()
         return out
 
+    @contextlib.contextmanager
+    def _mx_scope(self):
+        """The engine's device and stream, without gradients; not in inference mode, as the tensors of
+        average_mx are written outside it, too."""
+        torch = self.torch
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream), torch.inference_mode(False), torch.no_grad():
+            yield
+
     def average_mx(self, format: int = MX_E2M1, error_feedback: bool = True, products: bool = False):
         """The synchronization with microscaled messages in place of fp32 replicas: every worker sends
         its difference from mx_base, the model after the last sync (0 at first, as the replicas),
@@ -150,7 +159,7 @@ class Adpsgd:
         if self._mx_lost:
             raise AdpsgdError(ESTATE, "the workers' shared model has moved past mx_base: call mx_begin right behind a "
                                       "sync, or with the model after the last one")
-        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+        with self._mx_scope():
             if self.mx_base is None:
                 self.mx_base = torch.zeros((self.P,), device=self.device, dtype=torch.float32)
             if error_feedback and self.mx_residual is None:
@@ -188,7 +197,7 @@ class Adpsgd:
         if base is None and self.get_state().cnt != 0:
             raise ValueError("the workers have stepped on since the last sync: base must be given")
         self.stream.wait_stream(torch.cuda.current_stream(self.device))
-        with torch.cuda.device(self.device), torch.cuda.stream(self.stream), torch.no_grad():
+        with self._mx_scope():
             to_base, to_residual = self.mx_base, self.mx_residual
             if to_base is None:
                 to_base = torch.empty((self.P,), device=self.device, dtype=torch.float32)

@@ -260,6 +260,42 @@ def test_torchs_default_type_does_not_matter(A):
         torch.set_default_dtype(old)
 
 
+def test_inference_mode_does_not_matter(A):
+    """A sync inside it leaves the engine usable outside, and the other way round."""
+    w = _const(K=2)
+    zero = np.zeros((w.K, w.P), np.float32)
+    with A.Adpsgd.from_workload(w) as eng:
+        eng.local_steps(2)
+        with torch.inference_mode():
+            eng.average_mx()
+        eng.local_steps(2)
+        eng.average()
+        base = eng.x[0].cpu().numpy()
+        eng.local_steps(2)
+        with torch.inference_mode():
+            _sync_is_of(A, eng, w, base, zero)
+        eng.reset()
+        assert not eng.mx_base.any() and not eng.mx_residual.any()
+        with torch.inference_mode():
+            eng.mx_begin(torch.ones(w.P), torch.ones(w.K, w.P))
+        eng.mx_begin()
+        eng.local_steps(2)
+        _sync_is_of(A, eng, w, np.zeros(w.P, np.float32), zero)
+
+
+def test_replicas_that_require_gradients(A):
+    """The engine's syncs update them as an optimizer does."""
+    w = _const(K=2)
+    with A.Adpsgd.from_workload(w) as eng:
+        eng.x.requires_grad_()
+        eng.local_steps(2)
+        before = eng.x._version
+        eng.average_mx()
+        assert eng.x._version > before
+        eng.average()
+        eng.mx_begin()
+
+
 def test_engine_sync_of_a_larger_model(A):
     """Several chunks a tensor, tensors that share chunks, rows of many blocks."""
     import workloads as W
