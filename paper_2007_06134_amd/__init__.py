@@ -209,7 +209,7 @@ class Adpsgd:
             elif to_residual is not None:
                 to_residual.zero_()
             for t in (base, residual):         # (the caller may drop them before the copies have run)
-                if t is not None and t.is_cuda:
+                if t is not None and t.device == to_base.device:
                     t.record_stream(self.stream)
         self.mx_base, self.mx_residual, self._mx_lost = to_base, to_residual, False
 
